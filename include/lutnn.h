@@ -464,6 +464,95 @@ LUTNN_API lutnn_status lutnn_conv2d_tree(const lutnn_layer* layer, const lutnn_t
                                          void* stream);
 
 /*
+ * The layers that stand between looked-up ones in the same model: linear layers that stay dense, and layer norms.  Conventions
+ * as above, and:
+ *   - X, W, Y and every other matrix of a call have one type, `dtype`; vectors (bias, weight, statistics and their gradients)
+ *     are fp32.  Row strides are in elements, at least the width and at most 2^32.  A matrix is aligned to its values.
+ *   - Everything is computed in fp32 and rounded to `dtype` once, when it is stored; what else is rounded is said below.
+ *   - `workspace` is device memory of at least the bytes that the query names for the same arguments, 16-byte aligned, contents
+ *     unspecified before and after; it may be NULL where that is 0.
+ *   - Sums are taken in an order that the arguments alone decide: calls repeat bit for bit.
+ */
+typedef enum {
+    LUTNN_F32 = 0,
+    LUTNN_BF16 = 1,
+    LUTNN_F16 = 2
+} lutnn_dtype;
+
+typedef enum {
+    LUTNN_ACTIVATION_NONE = 0,
+    LUTNN_ACTIVATION_RELU = 1,      /* max(z, 0)                                             */
+    LUTNN_ACTIVATION_GELU = 2,      /* z/2 (1 + erf(z / sqrt 2))                             */
+    LUTNN_ACTIVATION_GELU_TANH = 3, /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))         */
+    LUTNN_ACTIVATION_SILU = 4       /* z / (1 + exp(-z))                                     */
+} lutnn_activation;
+
+/*
+ * A dense linear layer with its epilogue:  Z = X . W + bias,  Y = activation(Z) + residual.
+ *
+ *   X [N][D], W [D][M] (as lutnn_build_table), bias [M] fp32 or NULL, residual [N][M] or NULL
+ *   Y [N][M]; preactivation [N][M] or NULL: receives Z, which the backward pass of an activation needs
+ * D and M up to 2^24 - 512.  Errors: E_NULL, E_SHAPE, E_UNSUPPORTED (dtype, activation), E_ALIGN, E_HIP.
+ */
+LUTNN_API lutnn_status lutnn_dense_linear(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw,
+                                          int32_t D, int32_t M, const float* bias, int32_t activation, const void* residual,
+                                          int64_t ldr, void* Y, int64_t ldy, void* preactivation, int64_t ldz, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/* Host: bytes of workspace for lutnn_dense_linear on these operands (their addresses and strides matter, nothing is read); 0
+ * for what it refuses. */
+LUTNN_API size_t lutnn_dense_linear_workspace_bytes(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw,
+                                                    int32_t D, int32_t M);
+
+/*
+ * Its gradients from G = dL/dY:  dZ = G * activation'(Z),  dX = dZ . W^T,  dW = X^T . dZ,  dbias = the sum of dZ over its rows.
+ * The residual's gradient is G itself.  dZ is rounded to `dtype` before it is multiplied, as the operands of the products are;
+ * dbias is summed from what was not rounded.
+ *
+ *   G [N][M]; preactivation [N][M]: what the forward pass left; NULL without an activation
+ *   dX [N][D], dW [D][M], dbias [M] fp32: overwritten; any of them NULL to skip it.  X may be NULL without dW, W without dX.
+ *   N == 0: dW and dbias are zeros.
+ * Errors: as lutnn_dense_linear.
+ */
+LUTNN_API lutnn_status lutnn_dense_linear_backward(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw,
+                                                   int32_t D, int32_t M, const void* G, int64_t ldg, const void* preactivation,
+                                                   int64_t ldz, int32_t activation, void* dX, int64_t lddx, void* dW, int64_t lddw,
+                                                   float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+LUTNN_API size_t lutnn_dense_linear_backward_workspace_bytes(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W,
+                                                             int64_t ldw, int32_t D, int32_t M, const void* G, int64_t ldg,
+                                                             const void* preactivation, int64_t ldz, int32_t activation,
+                                                             int32_t need_dx, int32_t need_dw, int32_t need_dbias);
+
+/*
+ * Layer norm of the rows of S = X + residual:
+ *   mean = sum_d S[d] / D,  rstd = 1 / sqrt(sum_d (S[d] - mean)^2 / D + eps),  Y[d] = (S[d] - mean) rstd weight[d] + bias[d]
+ *
+ *   X [N][D], residual [N][D] or NULL, weight and bias [D] fp32 or NULL (ones, zeros), eps >= 0
+ *   Y [N][D]; total [N][D] or NULL: receives S (with a residual only); statistics [N][2] fp32 or NULL: receives mean and rstd
+ *   D up to 16384 (E_UNSUPPORTED above)
+ * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
+ */
+LUTNN_API lutnn_status lutnn_layer_norm(int32_t dtype, const void* X, int64_t N, int64_t ldx, int32_t D, const void* residual,
+                                        int64_t ldr, const float* weight, const float* bias, float eps, void* Y, int64_t ldy,
+                                        void* total, int64_t ldt, float* statistics, void* stream);
+
+/*
+ * Its gradients from G = dL/dY and from X, what was normalised (the forward pass's total, or its X without a residual):
+ *   h = (X - mean) rstd,  q = G weight:   dX = rstd (q - sum_d q / D - h sum_d (q h) / D) + residual,
+ *   dweight = sum_n G h,  dbias = sum_n G
+ *
+ *   residual [N][D] or NULL: a gradient that reaches X by another way, as where the total goes on beside the norm
+ *   dX [N][D], dweight [D], dbias [D] fp32: overwritten; any of them NULL to skip it.  N == 0: dweight and dbias are zeros.
+ *   workspace  needed for dweight and dbias
+ * Errors: as lutnn_layer_norm.
+ */
+LUTNN_API lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx,
+                                                 int32_t D, const float* statistics, const float* weight, const void* residual,
+                                                 int64_t ldr, void* dX, int64_t lddx, float* dweight, float* dbias, void* workspace,
+                                                 size_t workspace_bytes, void* stream);
+LUTNN_API size_t lutnn_layer_norm_backward_workspace_bytes(int64_t N, int32_t D);
+
+/*
  * Host: the variant that LUTNN_VARIANT_AUTO stands for in lutnn_lookup(layer, idx, N, ...) - and in
  * lutnn_linear when `idx` is its workspace - so that callers (and benchmarks) can report which
  * kernel ran.  Pure function of the descriptor, N and the address of idx; nothing is launched

@@ -38,7 +38,15 @@ EXPORTS = ["lutnn_softpq_backward_static", "lutnn_set_tunable", "lutnn_encode_tr
            "lutnn_auto_variant", "lutnn_linear_auto_variant", "lutnn_status_string", "lutnn_last_error", "lutnn_version",
            "lutnn_probe_smfmac_stream", "lutnn_linear_scratch", "lutnn_linear_tree_scratch", "lutnn_linear_scratch_bytes",
            "lutnn_conv2d_scratch_bytes", "lutnn_conv2d_scratch", "lutnn_conv2d_tree_scratch", "lutnn_bias_gradient",
-           "lutnn_bias_gradient_workspace_bytes", "lutnn_scratch_variant"]
+           "lutnn_bias_gradient_workspace_bytes", "lutnn_scratch_variant", "lutnn_dense_linear",
+           "lutnn_dense_linear_workspace_bytes", "lutnn_dense_linear_backward", "lutnn_dense_linear_backward_workspace_bytes",
+           "lutnn_layer_norm", "lutnn_layer_norm_backward", "lutnn_layer_norm_backward_workspace_bytes"]
+
+# lutnn_dtype: the matrices of the layers that are not looked up
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+# lutnn_activation
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 class LutnnError(RuntimeError):
@@ -168,6 +176,23 @@ def _load():
     lib.lutnn_version.restype = ctypes.c_char_p
     lib.lutnn_set_tunable.restype = i32
     lib.lutnn_set_tunable.argtypes = [ctypes.c_char_p, ctypes.c_char_p]
+    size = ctypes.c_size_t
+    lib.lutnn_dense_linear.restype = i32
+    lib.lutnn_dense_linear.argtypes = [i32, vp, i64, i64, vp, i64, i32, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp, size, vp]
+    lib.lutnn_dense_linear_workspace_bytes.restype = size
+    lib.lutnn_dense_linear_workspace_bytes.argtypes = [i32, vp, i64, i64, vp, i64, i32, i32]
+    lib.lutnn_dense_linear_backward.restype = i32
+    lib.lutnn_dense_linear_backward.argtypes = [i32, vp, i64, i64, vp, i64, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp,
+                                                vp, size, vp]
+    lib.lutnn_dense_linear_backward_workspace_bytes.restype = size
+    lib.lutnn_dense_linear_backward_workspace_bytes.argtypes = [i32, vp, i64, i64, vp, i64, i32, i32, vp, i64, vp, i64, i32, i32,
+                                                                i32, i32]
+    lib.lutnn_layer_norm.restype = i32
+    lib.lutnn_layer_norm.argtypes = [i32, vp, i64, i64, i32, vp, i64, vp, vp, ctypes.c_float, vp, i64, vp, i64, vp, vp]
+    lib.lutnn_layer_norm_backward.restype = i32
+    lib.lutnn_layer_norm_backward.argtypes = [i32, vp, i64, i64, vp, i64, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, size, vp]
+    lib.lutnn_layer_norm_backward_workspace_bytes.restype = size
+    lib.lutnn_layer_norm_backward_workspace_bytes.argtypes = [i64, i32]
     lib.lutnn_probe_smfmac_stream.restype = i32
     lib.lutnn_probe_smfmac_stream.argtypes = [i32, i32, vp, ctypes.c_size_t, vp]
     return lib
@@ -696,3 +721,132 @@ def linear(layer, X, variant="auto", out=None, idx_workspace=None):
     _check(LIB.lutnn_linear(layer.ref, _ptr(X), N, X.stride(0), _ptr(out),
                             out.stride(0), v, _ptr(idx_workspace), _stream()))
     return out
+
+
+# ---- the layers between the looked-up ones: dense linear layers and layer norms
+
+def _matrix(name, t, shape, like):
+    """Checks a matrix of a call whose type and device are those of `like`; its row stride (a single row has none)."""
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError("%s is %s on %s, expected %s on %s" % (name, t.dtype, t.device, like.dtype, like.device))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if shape[1] > 1 and shape[0] > 0 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _vector(name, t, length, like):
+    if t.dtype != torch.float32 or t.device != like.device or not t.is_contiguous() or tuple(t.shape) != (length,):
+        raise ValueError("%s must be a contiguous fp32 vector of %d values on %s" % (name, length, like.device))
+
+
+def _typed(name, t):
+    """lutnn_dtype of a call's first matrix."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype not in DTYPES:
+        raise ValueError("%s must be a CUDA matrix of fp32, bf16 or fp16" % name)
+    return DTYPES[t.dtype]
+
+
+def _activation(activation):
+    if activation not in ACTIVATIONS:
+        raise ValueError("unknown activation %r: %s" % (activation, ", ".join(repr(a) for a in ACTIVATIONS)))
+    return ACTIVATIONS[activation]
+
+
+def _workspace(nbytes, like):
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+def dense_linear(X, W, bias=None, activation=None, residual=None, out=None, preactivation=None):
+    """lutnn_dense_linear: Y = activation(X @ W + bias) + residual.  X [N, D], W [D, M] and residual [N, M] of one type (fp32,
+    bf16, fp16), bias [M] fp32; activation None, "relu", "gelu", "gelu_tanh" or "silu".  preactivation: an [N, M] tensor that
+    receives X @ W + bias, as dense_linear_backward wants it."""
+    dtype, act = _typed("X", X), _activation(activation)
+    (N, D), M = X.shape, W.shape[-1]
+    ldx, ldw = _matrix("X", X, (N, D), X), _matrix("W", W, (D, M), X)
+    ldr = 0 if residual is None else _matrix("residual", residual, (N, M), X)
+    ldz = 0 if preactivation is None else _matrix("preactivation", preactivation, (N, M), X)
+    if bias is not None:
+        _vector("bias", bias, M, X)
+    if out is None:
+        out = torch.empty((N, M), dtype=X.dtype, device=X.device)
+    ldy = _matrix("out", out, (N, M), X)
+    with torch.cuda.device(X.device):
+        nbytes = LIB.lutnn_dense_linear_workspace_bytes(dtype, _ptr(X), N, ldx, _ptr(W), ldw, D, M)
+        workspace = _workspace(nbytes, X)
+        _check(LIB.lutnn_dense_linear(dtype, _ptr(X), N, ldx, _ptr(W), ldw, D, M, _ptr(bias), act, _ptr(residual), ldr, _ptr(out),
+                                      ldy, _ptr(preactivation), ldz, _ptr(workspace), nbytes, _stream()))
+    return out
+
+
+def dense_linear_backward(X, W, G, preactivation=None, activation=None, need_dx=True, need_dw=True, need_dbias=True):
+    """lutnn_dense_linear_backward: the gradients of dense_linear from G = dL/dY [N, M].  Returns (dX [N, D], dW [D, M], dbias [M]
+    fp32), None for what is not needed.  The residual's gradient is G itself."""
+    dtype, act = _typed("G", G), _activation(activation)
+    (N, M), D = G.shape, W.shape[0]
+    ldx, ldw, ldg = _matrix("X", X, (N, D), G), _matrix("W", W, (D, M), G), _matrix("G", G, (N, M), G)
+    if act and preactivation is None:
+        raise ValueError("an activation's gradient needs the preactivation")
+    ldz = _matrix("preactivation", preactivation, (N, M), G) if act else 0
+    z = _ptr(preactivation) if act else None
+    dX = torch.empty((N, D), dtype=G.dtype, device=G.device) if need_dx else None
+    dW = torch.empty((D, M), dtype=G.dtype, device=G.device) if need_dw else None
+    db = torch.empty(M, dtype=torch.float32, device=G.device) if need_dbias else None
+    with torch.cuda.device(G.device):
+        nbytes = LIB.lutnn_dense_linear_backward_workspace_bytes(dtype, _ptr(X), N, ldx, _ptr(W), ldw, D, M, _ptr(G), ldg, z, ldz,
+                                                                 act, need_dx, need_dw, need_dbias)
+        workspace = _workspace(nbytes, G)
+        _check(LIB.lutnn_dense_linear_backward(dtype, _ptr(X), N, ldx, _ptr(W), ldw, D, M, _ptr(G), ldg, z, ldz, act, _ptr(dX), D,
+                                               _ptr(dW), M, _ptr(db), _ptr(workspace), nbytes, _stream()))
+    return dX, dW, db
+
+
+def layer_norm(X, weight=None, bias=None, eps=1e-5, residual=None, out=None, total=None, statistics=None):
+    """lutnn_layer_norm: the rows of S = X + residual, normalised, times weight, plus bias.  X [N, D] and residual of one type
+    (fp32, bf16, fp16), weight and bias [D] fp32.  total: an [N, D] tensor that receives S; statistics: an [N, 2] fp32 tensor that
+    receives the rows' mean and 1 / sqrt(variance + eps), as layer_norm_backward wants them."""
+    dtype = _typed("X", X)
+    N, D = X.shape
+    ldx = _matrix("X", X, (N, D), X)
+    ldr = 0 if residual is None else _matrix("residual", residual, (N, D), X)
+    ldt = 0 if total is None else _matrix("total", total, (N, D), X)
+    for name, v in (("weight", weight), ("bias", bias)):
+        if v is not None:
+            _vector(name, v, D, X)
+    if statistics is not None:
+        _statistics(statistics, X)
+    if out is None:
+        out = torch.empty((N, D), dtype=X.dtype, device=X.device)
+    ldy = _matrix("out", out, (N, D), X)
+    with torch.cuda.device(X.device):
+        _check(LIB.lutnn_layer_norm(dtype, _ptr(X), N, ldx, D, _ptr(residual), ldr, _ptr(weight), _ptr(bias), eps, _ptr(out), ldy,
+                                    _ptr(total), ldt, _ptr(statistics), _stream()))
+    return out
+
+
+def _statistics(t, like):
+    if t.dtype != torch.float32 or t.device != like.device or not t.is_contiguous() or tuple(t.shape) != (like.shape[0], 2):
+        raise ValueError("statistics must be a contiguous fp32 matrix of %d x 2 on %s" % (like.shape[0], like.device))
+
+
+def layer_norm_backward(G, X, statistics, weight=None, residual=None, need_dx=True, need_dweight=True, need_dbias=True):
+    """lutnn_layer_norm_backward: the gradients of layer_norm from G = dL/dY [N, D]; X is what was normalised (the total, where
+    there was a residual).  residual: a gradient [N, D] that reaches X by another way and is added to dX.  Returns (dX [N, D],
+    dweight [D], dbias [D]), the vectors fp32, None for what is not needed."""
+    dtype = _typed("G", G)
+    N, D = G.shape
+    ldg, ldx = _matrix("G", G, (N, D), G), _matrix("X", X, (N, D), G)
+    ldr = 0 if residual is None else _matrix("residual", residual, (N, D), G)
+    _statistics(statistics, G)
+    if weight is not None:
+        _vector("weight", weight, D, G)
+    dX = torch.empty((N, D), dtype=G.dtype, device=G.device) if need_dx else None
+    dw = torch.empty(D, dtype=torch.float32, device=G.device) if need_dweight else None
+    db = torch.empty(D, dtype=torch.float32, device=G.device) if need_dbias else None
+    with torch.cuda.device(G.device):
+        nbytes = LIB.lutnn_layer_norm_backward_workspace_bytes(N, D) if need_dweight or need_dbias else 0
+        workspace = _workspace(nbytes, G)
+        _check(LIB.lutnn_layer_norm_backward(dtype, _ptr(G), N, ldg, _ptr(X), ldx, D, _ptr(statistics), _ptr(weight), _ptr(residual),
+                                             ldr, _ptr(dX), D, _ptr(dw), _ptr(db), _ptr(workspace), nbytes, _stream()))
+    return dX, dw, db

@@ -1046,6 +1046,182 @@ lutnn_status lutnn_conv2d(const lutnn_layer* layer, const float* input, int64_t 
     return do_lookup(layer, v, idx_workspace, layer->C, N, Y, ldy, s);
 }
 
+}  // extern "C"
+
+// ---- the layers around the looked-up ones
+namespace {
+
+constexpr int kMaxWidth = (1 << 24) - 512;  // as check_dims
+
+int value_bytes(int32_t dtype) { return dtype == LUTNN_F32 ? 4 : 2; }
+
+lutnn_status check_dtype(int32_t dtype) {
+    if (dtype == LUTNN_F32 || dtype == LUTNN_BF16 || dtype == LUTNN_F16) return LUTNN_OK;
+    return fail(LUTNN_E_UNSUPPORTED, "unknown dtype %d", dtype);
+}
+
+lutnn_status check_rows(int64_t N) {
+    if (N < 0 || N >= kMaxRows) return fail(LUTNN_E_SHAPE, "N=%lld out of range", (long long)N);
+    return LUTNN_OK;
+}
+
+// A matrix of `width` columns with row stride ld: given where it is required, and its rows apart from each other.
+lutnn_status check_matrix(const char* name, const void* A, int64_t ld, int64_t width, int32_t dtype, bool required) {
+    if (!A) return required ? fail(LUTNN_E_NULL, "%s is NULL", name) : LUTNN_OK;
+    if (ld < width)
+        return fail(LUTNN_E_SHAPE, "the row stride %lld of %s is smaller than its width %lld", (long long)ld, name, (long long)width);
+    if (ld > ((int64_t)1 << 32)) return fail(LUTNN_E_SHAPE, "the row stride %lld of %s is larger than 2^32", (long long)ld, name);
+    if (!aligned(A, value_bytes(dtype)))
+        return fail(LUTNN_E_ALIGN, "%s must be aligned to its values' %d bytes", name, value_bytes(dtype));
+    return LUTNN_OK;
+}
+
+lutnn_status check_vector(const char* name, const float* v) {
+    if (!aligned(v, 4)) return fail(LUTNN_E_ALIGN, "%s must be 4-byte aligned", name);
+    return LUTNN_OK;
+}
+
+lutnn_status check_dense(int32_t dtype, int64_t N, int32_t D, int32_t M, int32_t activation) {
+    if (lutnn_status st = check_dtype(dtype)) return st;
+    if (activation < LUTNN_ACTIVATION_NONE || activation > LUTNN_ACTIVATION_SILU)
+        return fail(LUTNN_E_UNSUPPORTED, "unknown activation %d", activation);
+    if (D <= 0 || M <= 0 || D > kMaxWidth || M > kMaxWidth) return fail(LUTNN_E_SHAPE, "D=%d or M=%d out of range", D, M);
+    return check_rows(N);
+}
+
+lutnn_status check_workspace(const void* workspace, size_t given, size_t needed) {
+    if (needed == 0) return LUTNN_OK;
+    if (!workspace) return fail(LUTNN_E_NULL, "workspace is NULL");
+    if (given < needed)
+        return fail(LUTNN_E_SHAPE, "workspace of %zu bytes is smaller than the %zu this call needs", given, needed);
+    if (!aligned(workspace, 16)) return fail(LUTNN_E_ALIGN, "workspace must be 16-byte aligned");
+    return LUTNN_OK;
+}
+
+lutnn_status check_norm(int32_t dtype, int64_t N, int32_t D) {
+    if (lutnn_status st = check_dtype(dtype)) return st;
+    if (D <= 0) return fail(LUTNN_E_SHAPE, "D=%d must be positive", D);
+    if (D > lutnn::kMaxNormWidth) return fail(LUTNN_E_UNSUPPORTED, "rows of D=%d values: %d at most", D, lutnn::kMaxNormWidth);
+    return check_rows(N);
+}
+
+// the first check that fails
+template <class... Checks>
+lutnn_status first_failure(Checks&&... checks) {
+    lutnn_status st = LUTNN_OK;
+    (void)((st = checks(), st == LUTNN_OK) && ...);
+    return st;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lutnn_dense_linear_workspace_bytes(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int32_t D,
+                                          int32_t M) {
+    if (check_dense(dtype, N, D, M, LUTNN_ACTIVATION_NONE) || N == 0 || ldx < D || ldw < M) return 0;
+    return lutnn::dense_linear_workspace({dtype, X, N, ldx, W, ldw, D, M});
+}
+
+lutnn_status lutnn_dense_linear(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int32_t D, int32_t M,
+                                const float* bias, int32_t activation, const void* residual, int64_t ldr, void* Y, int64_t ldy,
+                                void* preactivation, int64_t ldz, void* workspace, size_t workspace_bytes, void* stream) {
+    if (lutnn_status st = check_dense(dtype, N, D, M, activation)) return st;
+    if (N == 0) return LUTNN_OK;
+    if (lutnn_status st = first_failure([&] { return check_matrix("X", X, ldx, D, dtype, true); },
+                                        [&] { return check_matrix("W", W, ldw, M, dtype, true); },
+                                        [&] { return check_matrix("residual", residual, ldr, M, dtype, false); },
+                                        [&] { return check_matrix("Y", Y, ldy, M, dtype, true); },
+                                        [&] { return check_matrix("preactivation", preactivation, ldz, M, dtype, false); },
+                                        [&] { return check_vector("bias", bias); }))
+        return st;
+    const lutnn::DenseCall call = {dtype, X, N, ldx, W, ldw, D, M};
+    if (lutnn_status st = check_workspace(workspace, workspace_bytes, lutnn::dense_linear_workspace(call))) return st;
+    return hip_result(lutnn::launch_dense_linear(call, bias, activation, residual, ldr, Y, ldy, preactivation, ldz, workspace,
+                                                 static_cast<hipStream_t>(stream)),
+                      "dense linear launch");
+}
+
+size_t lutnn_dense_linear_backward_workspace_bytes(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw,
+                                                   int32_t D, int32_t M, const void* G, int64_t ldg, const void* preactivation,
+                                                   int64_t ldz, int32_t activation, int32_t need_dx, int32_t need_dw,
+                                                   int32_t need_dbias) {
+    if (check_dense(dtype, N, D, M, activation) || N == 0) return 0;
+    if (ldg < M || (activation && ldz < M) || (need_dx && ldw < M) || (need_dw && ldx < D)) return 0;
+    return lutnn::dense_linear_gradient_workspace({dtype, X, N, ldx, W, ldw, D, M}, G, ldg, preactivation, ldz, activation,
+                                                  need_dx != 0, need_dw != 0, need_dbias != 0);
+}
+
+lutnn_status lutnn_dense_linear_backward(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int32_t D,
+                                         int32_t M, const void* G, int64_t ldg, const void* preactivation, int64_t ldz,
+                                         int32_t activation, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+    if (lutnn_status st = check_dense(dtype, N, D, M, activation)) return st;
+    if (lutnn_status st = first_failure([&] { return check_matrix("X", X, ldx, D, dtype, dW && N > 0); },
+                                        [&] { return check_matrix("W", W, ldw, M, dtype, dX && N > 0); },
+                                        [&] { return check_matrix("G", G, ldg, M, dtype, N > 0); },
+                                        [&] { return check_matrix("preactivation", preactivation, ldz, M, dtype, activation && N > 0); },
+                                        [&] { return check_matrix("dX", dX, lddx, D, dtype, false); },
+                                        [&] { return check_matrix("dW", dW, lddw, M, dtype, false); },
+                                        [&] { return check_vector("dbias", dbias); }))
+        return st;
+    const lutnn::DenseCall call = {dtype, X, N, ldx, W, ldw, D, M};
+    if (N > 0)
+        if (lutnn_status st = check_workspace(workspace, workspace_bytes,
+                                              lutnn::dense_linear_gradient_workspace(call, G, ldg, preactivation, ldz, activation,
+                                                                                     dX != nullptr, dW != nullptr, dbias != nullptr)))
+            return st;
+    return hip_result(lutnn::launch_dense_linear_gradient(call, G, ldg, preactivation, ldz, activation, dX, lddx, dW, lddw, dbias,
+                                                          workspace, static_cast<hipStream_t>(stream)),
+                      "dense linear gradient launch");
+}
+
+lutnn_status lutnn_layer_norm(int32_t dtype, const void* X, int64_t N, int64_t ldx, int32_t D, const void* residual, int64_t ldr,
+                              const float* weight, const float* bias, float eps, void* Y, int64_t ldy, void* total, int64_t ldt,
+                              float* statistics, void* stream) {
+    if (lutnn_status st = check_norm(dtype, N, D)) return st;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(LUTNN_E_SHAPE, "eps=%g must be finite and not negative", (double)eps);
+    if (N == 0) return LUTNN_OK;
+    if (total && !residual) return fail(LUTNN_E_NULL, "a total without a residual is X itself");
+    if (lutnn_status st = first_failure([&] { return check_matrix("X", X, ldx, D, dtype, true); },
+                                        [&] { return check_matrix("residual", residual, ldr, D, dtype, false); },
+                                        [&] { return check_matrix("Y", Y, ldy, D, dtype, true); },
+                                        [&] { return check_matrix("total", total, ldt, D, dtype, false); },
+                                        [&] { return check_vector("weight", weight); }, [&] { return check_vector("bias", bias); },
+                                        [&] { return check_vector("statistics", statistics); }))
+        return st;
+    return hip_result(lutnn::launch_layer_norm(dtype, X, N, ldx, D, residual, ldr, weight, bias, eps, Y, ldy, total, ldt, statistics,
+                                               static_cast<hipStream_t>(stream)),
+                      "layer norm launch");
+}
+
+size_t lutnn_layer_norm_backward_workspace_bytes(int64_t N, int32_t D) {
+    if (check_norm(LUTNN_F32, N, D) || N == 0) return 0;
+    return lutnn::layer_norm_gradient_workspace(N, D);
+}
+
+lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int32_t D,
+                                       const float* statistics, const float* weight, const void* residual, int64_t ldr, void* dX,
+                                       int64_t lddx, float* dweight, float* dbias, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
+    if (lutnn_status st = check_norm(dtype, N, D)) return st;
+    if (N > 0 && !statistics) return fail(LUTNN_E_NULL, "statistics is NULL");
+    if (lutnn_status st = first_failure([&] { return check_matrix("G", G, ldg, D, dtype, N > 0); },
+                                        [&] { return check_matrix("X", X, ldx, D, dtype, N > 0); },
+                                        [&] { return check_matrix("residual", residual, ldr, D, dtype, false); },
+                                        [&] { return check_matrix("dX", dX, lddx, D, dtype, false); },
+                                        [&] { return check_vector("statistics", statistics); },
+                                        [&] { return check_vector("weight", weight); }, [&] { return check_vector("dweight", dweight); },
+                                        [&] { return check_vector("dbias", dbias); }))
+        return st;
+    if (dweight || dbias)
+        if (lutnn_status st = check_workspace(workspace, workspace_bytes, N > 0 ? lutnn::layer_norm_gradient_workspace(N, D) : 0)) return st;
+    if (!dX && !dweight && !dbias) return LUTNN_OK;
+    return hip_result(lutnn::launch_layer_norm_gradient(dtype, G, N, ldg, X, ldx, D, statistics, weight, residual, ldr, dX, lddx,
+                                                        dweight, dbias, workspace, static_cast<hipStream_t>(stream)),
+                      "layer norm gradient launch");
+}
+
 int32_t lutnn_auto_variant(const lutnn_layer* layer, const uint8_t* idx, int64_t N) {
     if (!layer) return -1;
     return resolve_lookup_variant(layer, LUTNN_VARIANT_AUTO, idx, N);

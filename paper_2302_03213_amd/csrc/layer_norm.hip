@@ -1,0 +1,308 @@
+// Layer norm over the rows of a matrix, forward and backward: the normalisations between the linear layers of a model, whether
+// those are looked up in tables or dense.
+//
+//   s = x + r          mu = sum s / D          rstd = 1 / sqrt(sum (s - mu)^2 / D + eps)          y = (s - mu) rstd w + b
+//   h = (x - mu) rstd, q = g w:   dx = rstd (q - sum q / D - h sum (q h) / D) + r,   dw = sum_n g h,   db = sum_n g
+//
+// What bounds both: every matrix read or written once, at the rate of the memory.  A row lies in the registers of the threads
+// that share it, 16 values each, so that nothing is read twice: the sum of squares is that of the differences from the mean (two
+// reductions of a row, no cancellation).  Rows of up to 256 values take 16 threads, up to 1024 a wavefront, up to 4096 four, up
+// to 16384 sixteen.  Sums are fp32 ones.
+#include <algorithm>
+
+#include "lutnn_kernels.h"
+#include "matrix_types.h"
+
+namespace lutnn {
+namespace {
+
+constexpr int kValues = 16;     // of a row, per thread
+constexpr int kThreads = 256;   // per workgroup, but for rows that take more
+
+template <class T>
+constexpr int kVector = 16 / sizeof(T);  // values per load
+
+// A row's values as `TPR` threads hold them: vector c of thread t starts at column (c * TPR + t) * VEC.  The last vector of a row
+// that is no whole number of them is moved back to end with it; what it then repeats of its neighbour's counts as zero in sums
+// and is stored twice, with the same value.
+template <int VEC, int TPR>
+struct Columns {
+    int D, t;
+    __device__ __forceinline__ int start(int c) const { return (c * TPR + t) * VEC; }
+    __device__ __forceinline__ bool any(int c) const { return start(c) < D; }
+    __device__ __forceinline__ int at(int c) const { return min(start(c), D - VEC); }
+    __device__ __forceinline__ bool mine(int c, int j) const { return at(c) + j >= start(c); }
+};
+
+// The sums over a row's threads, in every one of them.  shared: 2 * count floats per wavefront, the halves in turn.
+template <int TPR, int count>
+__device__ __forceinline__ void row_sums(float (&v)[count], float* shared, int& turn) {
+#pragma unroll
+    for (int d = 1; d < (TPR < 64 ? TPR : 64); d *= 2)
+#pragma unroll
+        for (int i = 0; i < count; ++i) v[i] += __shfl_xor(v[i], d, 64);
+    if constexpr (TPR > 64) {
+        constexpr int kWaves = TPR / 64;
+        float* const slot = shared + turn * count * kWaves;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < count; ++i) slot[i * kWaves + (threadIdx.x >> 6)] = v[i];
+        __syncthreads();  // one is enough: a half is written again only behind the other half's barrier
+#pragma unroll
+        for (int i = 0; i < count; ++i) {
+            v[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v[i] += slot[i * kWaves + w];
+        }
+    }
+}
+
+template <class T>
+struct NormArgs {
+    const T *X, *R;
+    const float *w, *b;
+    T *Y, *S;
+    float* statistics;
+    int64_t N, ldx, ldr, ldy, lds;
+    int D;
+    float eps;
+};
+
+// grid: rows, kThreads / TPR (or one) of them per workgroup.
+template <class T, int VEC, int TPR>
+__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_kernel(NormArgs<T> a) {
+    constexpr int ROWS = TPR < kThreads ? kThreads / TPR : 1, CH = VEC == 1 ? 1 : kValues / VEC;
+    __shared__ float shared[2 * (TPR > 64 ? TPR / 64 : 1)];
+    int turn = 0;
+    const int64_t n = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (n >= a.N) return;  // whole wavefronts or, in groups of 16, nobody that the others wait for
+    const Columns<VEC, TPR> col{a.D, (int)(threadIdx.x % TPR)};
+    float x[CH][VEC], total[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        if (!col.any(c)) continue;
+        load_values(a.X + n * a.ldx + col.at(c), x[c]);
+        if (a.R) {
+            float r[VEC];
+            load_values(a.R + n * a.ldr + col.at(c), r);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[c][j] += r[j];
+            if (a.S) store_values(a.S + n * a.lds + col.at(c), x[c]);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) total[0] += col.mine(c, j) ? x[c][j] : 0.f;
+    }
+    row_sums<TPR>(total, shared, turn);
+    const float mean = total[0] / a.D;
+    float squares[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+        if (col.any(c))
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                x[c][j] -= mean;
+                squares[0] += col.mine(c, j) ? x[c][j] * x[c][j] : 0.f;
+            }
+    row_sums<TPR>(squares, shared, turn);
+    const float rstd = 1.f / sqrtf(squares[0] / a.D + a.eps);
+    if (a.statistics && col.t == 0) {
+        a.statistics[2 * n] = mean;
+        a.statistics[2 * n + 1] = rstd;
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        if (!col.any(c)) continue;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[c][j] *= rstd;
+        if (a.w) {
+            float w[VEC];
+            load_values(a.w + col.at(c), w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[c][j] *= w[j];
+        }
+        if (a.b) {
+            float b[VEC];
+            load_values(a.b + col.at(c), b);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[c][j] += b[j];
+        }
+        store_values(a.Y + n * a.ldy + col.at(c), x[c]);
+    }
+}
+
+template <class T>
+struct NormGradientArgs {
+    const T *G, *X, *R;
+    const float *statistics, *w;
+    T* dX;
+    float* partial;  // [workgroups][2][D]
+    int64_t N, ldg, ldx, ldr, lddx;
+    int D;
+};
+
+// Rows are dealt to the workgroups in turn; each keeps the column sums of its own in registers and leaves them in `partial`.
+template <class T, int VEC, int TPR>
+__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gradient_kernel(NormGradientArgs<T> a) {
+    constexpr int THREADS = TPR < kThreads ? kThreads : TPR, ROWS = THREADS / TPR, CH = VEC == 1 ? 1 : kValues / VEC;
+    __shared__ float shared[4 * (TPR > 64 ? TPR / 64 : 1)];
+    __shared__ float parts[ROWS > 1 ? CH * VEC * THREADS : 1];
+    int turn = 0;
+    const Columns<VEC, TPR> col{a.D, (int)(threadIdx.x % TPR)};
+    float dw[CH][VEC] = {}, db[CH][VEC] = {};
+    for (int64_t n = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; n < a.N; n += (int64_t)gridDim.x * ROWS) {
+        const float mean = a.statistics[2 * n], rstd = a.statistics[2 * n + 1];
+        float g[CH][VEC], h[CH][VEC], sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!col.any(c)) continue;
+            load_values(a.G + n * a.ldg + col.at(c), g[c]);
+            load_values(a.X + n * a.ldx + col.at(c), h[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!col.any(c)) continue;
+            float w[VEC];
+            if (a.w) load_values(a.w + col.at(c), w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                h[c][j] = (h[c][j] - mean) * rstd;
+                if (col.mine(c, j)) {
+                    dw[c][j] = __fmaf_rn(g[c][j], h[c][j], dw[c][j]);
+                    db[c][j] += g[c][j];
+                }
+                if (a.w) g[c][j] *= w[j];
+                sums[0] += col.mine(c, j) ? g[c][j] : 0.f;
+                sums[1] += col.mine(c, j) ? g[c][j] * h[c][j] : 0.f;
+            }
+        }
+        if (!a.dX) continue;
+        row_sums<TPR>(sums, shared, turn);
+        const float q = sums[0] / a.D, qh = sums[1] / a.D;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!col.any(c)) continue;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) g[c][j] = rstd * (g[c][j] - q - h[c][j] * qh);
+            if (a.R) {
+                float r[VEC];
+                load_values(a.R + n * a.ldr + col.at(c), r);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) g[c][j] += r[j];
+            }
+            store_values(a.dX + n * a.lddx + col.at(c), g[c]);
+        }
+    }
+    if (!a.partial) return;
+    const auto leave = [&](float(&v)[CH][VEC], float* to) {
+        if constexpr (ROWS > 1) {  // the workgroup's rows, in order
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) parts[(c * VEC + j) * THREADS + threadIdx.x] = v[c][j];
+            __syncthreads();
+            if (threadIdx.x >= TPR) return;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+#pragma unroll 1
+                    for (int r = 1; r < ROWS; ++r) v[c][j] += parts[(c * VEC + j) * THREADS + r * TPR + threadIdx.x];
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (col.any(c))
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    if (col.mine(c, j)) to[col.at(c) + j] = v[c][j];
+    };
+    float* const mine = a.partial + (int64_t)blockIdx.x * 2 * a.D;
+    leave(dw, mine);
+    leave(db, mine + a.D);
+}
+
+// out[d] = sum over the workgroups of partial[workgroup][d], for the 2 D columns of both gradients: 32 columns per workgroup, every
+// eighth partial sum per thread, 64-bit sums in a fixed order.
+__global__ __launch_bounds__(256) void norm_column_sums_kernel(const float* __restrict__ partial, int count, int D,
+                                                               float* __restrict__ dw, float* __restrict__ db) {
+    __shared__ double part[8][32];
+    const int i = threadIdx.x & 31, group = threadIdx.x >> 5, d = blockIdx.x * 32 + i;
+    double sum = 0;
+    if (d < 2 * D)
+        for (int k = group; k < count; k += 8) sum += partial[(int64_t)k * 2 * D + d];
+    part[group][i] = sum;
+    __syncthreads();
+    if (group != 0 || d >= 2 * D) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) sum += part[k][i];
+    float* const out = d < D ? dw : db;
+    if (out) out[d < D ? d : d - D] = (float)sum;
+}
+
+template <class T, class F>
+hipError_t by_width(int D, F&& f) {
+    using std::integral_constant;
+    constexpr int V = kVector<T>;
+    if (D < V) return f(integral_constant<int, 1>(), integral_constant<int, 16>());
+    if (D <= 16 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 16>());
+    if (D <= 64 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 64>());
+    if (D <= 256 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 256>());
+    return f(integral_constant<int, V>(), integral_constant<int, 1024>());
+}
+
+int rows_per_workgroup(int D) { return D <= 16 * kValues ? kThreads / 16 : D <= 64 * kValues ? kThreads / 64 : 1; }
+
+// Two workgroups per compute unit for a row of four wavefronts or less.
+int gradient_workgroups(int64_t N, int D) {
+    const int64_t most = (D <= 256 * kValues ? 2 : 1) * (int64_t)compute_units();
+    const int rows = rows_per_workgroup(D);
+    return (int)std::min<int64_t>((N + rows - 1) / rows, most);
+}
+
+}  // namespace
+
+size_t layer_norm_gradient_workspace(int64_t N, int D) { return (size_t)gradient_workgroups(N, D) * 2 * D * sizeof(float); }
+
+hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
+                             const float* b, float eps, void* Y, int64_t ldy, void* S, int64_t lds, float* statistics,
+                             hipStream_t s) {
+    return with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        const NormArgs<T> a{static_cast<const T*>(X), static_cast<const T*>(R), w, b, static_cast<T*>(Y), static_cast<T*>(S),
+                            statistics, N, ldx, ldr, ldy, lds, D, eps};
+        return by_width<T>(D, [&](auto vec, auto tpr) {
+            constexpr int TPR = decltype(tpr)::value, ROWS = TPR < kThreads ? kThreads / TPR : 1;
+            hipLaunchKernelGGL((layer_norm_kernel<T, decltype(vec)::value, TPR>), dim3((unsigned)((N + ROWS - 1) / ROWS)),
+                               dim3(TPR < kThreads ? kThreads : TPR), 0, s, a);
+            return hipGetLastError();
+        });
+    });
+}
+
+hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
+                                      const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
+                                      float* dw, float* db, void* workspace, hipStream_t s) {
+    float* const partial = dw || db ? static_cast<float*>(workspace) : nullptr;
+    const int groups = gradient_workgroups(N, D);
+    if (groups > 0) {
+        const hipError_t e = with_type(dtype, [&](auto t) {
+            using T = decltype(t);
+            const NormGradientArgs<T> a{static_cast<const T*>(G), static_cast<const T*>(X), static_cast<const T*>(R), statistics, w,
+                                        static_cast<T*>(dX), partial, N, ldg, ldx, ldr, lddx, D};
+            return by_width<T>(D, [&](auto vec, auto tpr) {
+                constexpr int TPR = decltype(tpr)::value;
+                hipLaunchKernelGGL((layer_norm_gradient_kernel<T, decltype(vec)::value, TPR>), dim3((unsigned)groups),
+                                   dim3(TPR < kThreads ? kThreads : TPR), 0, s, a);
+                return hipGetLastError();
+            });
+        });
+        if (e != hipSuccess) return e;
+    }
+    if (!dw && !db) return hipSuccess;
+    hipLaunchKernelGGL(norm_column_sums_kernel, dim3((unsigned)((2 * D + 31) / 32)), dim3(256), 0, s,
+                       static_cast<const float*>(workspace), groups, D, dw, db);
+    return hipGetLastError();
+}
+
+}  // namespace lutnn

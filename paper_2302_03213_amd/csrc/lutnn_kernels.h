@@ -198,6 +198,36 @@ hipError_t launch_linear_small_tree(const int32_t* split_dim, const float* thres
                                     int table_kind, const float* scale, const float* bias, int C, int V, int M,
                                     const float* X, int64_t N, int64_t ldx, float* Y, int64_t ldy, hipStream_t s);
 
+// dense_linear.hip: a linear layer that is not looked up, Y = act(X W + b) + R, and its gradients.  dtype: lutnn_dtype;
+// activation: lutnn_activation.  Workspaces are 16-byte aligned.
+struct DenseCall {
+    int dtype;
+    const void* X;
+    int64_t N, ldx;
+    const void* W;
+    int64_t ldw;
+    int D, M;
+};
+size_t dense_linear_workspace(const DenseCall& c);
+hipError_t launch_dense_linear(const DenseCall& c, const float* bias, int activation, const void* R, int64_t ldr, void* Y,
+                               int64_t ldy, void* Z, int64_t ldz, void* workspace, hipStream_t s);
+// G: dL/dY; Z: X W + b, looked at where there is an activation; any of dX, dW, db may be missing
+size_t dense_linear_gradient_workspace(const DenseCall& c, const void* G, int64_t ldg, const void* Z, int64_t ldz, int activation,
+                                       bool need_dx, bool need_dw, bool need_db);
+hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64_t ldg, const void* Z, int64_t ldz, int activation,
+                                        void* dX, int64_t lddx, void* dW, int64_t lddw, float* db, void* workspace,
+                                        hipStream_t s);
+
+// layer_norm.hip: rows of 1 .. kMaxNormWidth values
+constexpr int kMaxNormWidth = 16384;
+hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
+                             const float* b, float eps, void* Y, int64_t ldy, void* S, int64_t lds, float* statistics,
+                             hipStream_t s);
+size_t layer_norm_gradient_workspace(int64_t N, int D);
+hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
+                                      const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
+                                      float* dw, float* db, void* workspace, hipStream_t s);
+
 // probe_smfmac.hip: sink holds 256 * compute_units() ints
 hipError_t launch_probe_smfmac_stream(int operands, int iterations, int32_t* sink, hipStream_t s);
 
