@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 namespace lutnn {
 
 enum Activation { kActNone = 0, kActRelu, kActGelu, kActGeluTanh, kActSilu };
@@ -38,6 +40,34 @@ __device__ __forceinline__ float slope(float z, int activation) {
         }
         default: return 1.f;
     }
+}
+
+// Calls f with the activation as a constant; not at all for none.
+template <class F>
+__device__ __forceinline__ void with_activation(int activation, F&& f) {
+    switch (activation) {
+        case kActRelu: return f(std::integral_constant<int, kActRelu>());
+        case kActGelu: return f(std::integral_constant<int, kActGelu>());
+        case kActGeluTanh: return f(std::integral_constant<int, kActGeluTanh>());
+        case kActSilu: return f(std::integral_constant<int, kActSilu>());
+    }
+}
+
+template <int n>
+__device__ __forceinline__ void activate_all(float (&z)[n], int activation) {
+    with_activation(activation, [&](auto kind) {
+#pragma unroll
+        for (int r = 0; r < n; ++r) z[r] = activate(z[r], decltype(kind)::value);
+    });
+}
+
+// g times the slopes at z
+template <int n>
+__device__ __forceinline__ void slope_all(float (&g)[n], const float (&z)[n], int activation) {
+    with_activation(activation, [&](auto kind) {
+#pragma unroll
+        for (int r = 0; r < n; ++r) g[r] *= slope(z[r], decltype(kind)::value);
+    });
 }
 
 }  // namespace lutnn

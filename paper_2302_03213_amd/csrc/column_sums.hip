@@ -183,6 +183,26 @@ __global__ __launch_bounds__(32 * kGroups) void share_sums_kernel(const f64* __r
     out[m] = (float)sum;
 }
 
+// out[m] = sum over k of partial[k][m], the columns from `first` on to `rest` instead: 32 columns per workgroup, every 32nd sum per
+// thread, 64-bit sums.
+__global__ __launch_bounds__(1024) void partial_sums_kernel(const float* __restrict__ partial, int count, int64_t width,
+                                                            int64_t first, float* __restrict__ out, float* __restrict__ rest) {
+    __shared__ double part[32][33];
+    const int i = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const int64_t m = blockIdx.x * 32LL + i;
+    double sum = 0;
+    if (m < width)
+#pragma unroll 8
+        for (int k = group; k < count; k += 32) sum += partial[k * width + m];
+    part[group][i] = sum;
+    __syncthreads();
+    if (group != 0 || m >= width) return;
+#pragma unroll
+    for (int k = 1; k < 32; ++k) sum += part[k][i];
+    float* const to = m < first ? out : rest;
+    if (to) to[m < first ? m : m - first] = (float)sum;
+}
+
 struct Shares {
     int64_t count = 1;
     int lpr, col_tiles;           // rows
@@ -231,6 +251,13 @@ size_t column_sums_workspace(int64_t outer, int M, int64_t inner) {
     const size_t sums = (size_t)share_out(outer, M, inner).count * M * sizeof(double);
     // never less than the float per plane that the first form of these kernels took
     return std::max(sums, inner > 1 ? (size_t)outer * M * sizeof(float) : (size_t)0);
+}
+
+hipError_t launch_partial_sums(const float* partial, int count, int64_t width, int64_t first, float* out, float* rest,
+                               hipStream_t s) {
+    hipLaunchKernelGGL(partial_sums_kernel, dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, s, partial, count, width, first,
+                       out, rest);
+    return hipGetLastError();
 }
 
 hipError_t launch_column_sums(const float* G, int64_t outer, int64_t ldg, int M, int64_t inner, void* workspace, float* out,

@@ -1,137 +1,315 @@
 // Linear layers that are not looked up: Y = act(X W + b) + R, and the gradients of X, W and b.
 //
 //   Z = X W + b,  Y = act(Z) + R;      dZ = dL/dY act'(Z),  dX = dZ W^T,  dW = X^T dZ,  db = sum over rows of dZ
-#include "activation.h"
-#include "lutnn_kernels.h"
-#include "matrix_types.h"
+//
+// The three products run on the matrix cores (dense_product.h), which want 16-bit operands whose rows are whole aligned 16-byte
+// vectors.  Matrices that are such go to them as they are; others are laid out in the workspace first: fp32 ones as three planes of
+// bf16 parts, 16-bit ones of odd widths, strides or addresses as copies with padded rows.  dZ is formed on the way there, and summed
+// for db in the same pass.
+#include <algorithm>
+#include <type_traits>
+
+#include "dense_product.h"
 
 namespace lutnn {
 namespace {
 
-constexpr int kTile = 64, kDepth = 16;
+constexpr int kVec = 8;                      // columns per thread of the passes over a matrix
+constexpr int64_t kMaxStride = 1 << 21;      // values: a tile's rows within 32-bit offsets
 
-struct Epilogue {
-    const float* bias;
-    int activation;
-    const void* R;
-    void* Y;
-    void* Z;
-    int64_t ldr, ldy, ldz;
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+bool usable(int dtype, const void* p, int64_t ld, int64_t width) {
+    return dtype != 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= kMaxStride;
+}
+
+int64_t laid_out_stride(int64_t width) { return round_up(width, 8); }
+size_t laid_out_bytes(int dtype, int64_t rows, int64_t width) {
+    return (size_t)round_up((dtype == 0 ? 3 : 1) * rows * laid_out_stride(width) * 2, 256);
+}
+
+// in kernels
+__device__ __forceinline__ int64_t round8(int64_t width) { return (width + 7) / 8 * 8; }
+__device__ __forceinline__ int64_t laid_out_units(int64_t width) { return (width + kVec - 1) / kVec; }
+
+// Eight values of a row, those past its end as zeros.
+template <class T>
+__device__ __forceinline__ void load_row(const T* row, int64_t col, int64_t width, float (&v)[kVec]) {
+    if (col + kVec <= width) {
+        load_values(row + col, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = col + i < width ? (float)row[col + i] : 0.f;
+}
+
+// Eight values to where the matrix cores read them: fp32 ones as their parts.
+template <class T>
+__device__ __forceinline__ void lay_out(const float (&v)[kVec], uint16_t* to, int64_t plane) {
+    if constexpr (sizeof(T) == 4) {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        uint32_t bits[kVec], high[4], mid[4], low[4];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) bits[i] = __float_as_uint(v[i]);
+        cut<4>(bits, high, mid, low);
+        *reinterpret_cast<u32x4*>(to) = u32x4{high[0], high[1], high[2], high[3]};
+        *reinterpret_cast<u32x4*>(to + plane) = u32x4{mid[0], mid[1], mid[2], mid[3]};
+        *reinterpret_cast<u32x4*>(to + 2 * plane) = u32x4{low[0], low[1], low[2], low[3]};
+    } else {
+        store_values(reinterpret_cast<T*>(to), v);
+    }
+}
+
+// Up to two matrices laid out in one launch.
+struct LayOut {
+    const void* from[2];
+    int64_t ld[2], rows[2], width[2];
+    uint16_t* to[2];
 };
 
-// C[i][j] = sum_k A[i * ai + k * ak] * B[k * bk + j * bj]
 template <class T>
-__global__ __launch_bounds__(256) void product_kernel(const T* __restrict__ A, int64_t ai, int64_t ak, const T* __restrict__ B,
-                                                      int64_t bk, int64_t bj, int64_t I, int J, int64_t K, int j_tiles,
-                                                      Epilogue e) {
-    __shared__ float a[kDepth][kTile + 4], b[kDepth][kTile + 4];
-    const int64_t i0 = (int64_t)(blockIdx.x / j_tiles) * kTile;
-    const int j0 = (int)(blockIdx.x % j_tiles) * kTile;
-    const int ti = threadIdx.x / 16 * 4, tj = threadIdx.x % 16 * 4;
-    float sum[4][4] = {};
-    for (int64_t k0 = 0; k0 < K; k0 += kDepth) {
-        for (int v = threadIdx.x; v < kTile * kDepth; v += 256) {
-            const int ia = ak == 1 ? v / kDepth : v % kTile, ka = ak == 1 ? v % kDepth : v / kTile;
-            a[ka][ia] = i0 + ia < I && k0 + ka < K ? (float)A[(i0 + ia) * ai + (k0 + ka) * ak] : 0.f;
-            const int jb = bk == 1 ? v / kDepth : v % kTile, kb = bk == 1 ? v % kDepth : v / kTile;
-            b[kb][jb] = j0 + jb < J && k0 + kb < K ? (float)B[(k0 + kb) * bk + (j0 + jb) * bj] : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[i][j] = __fmaf_rn(a[k][ti + i], b[k][tj + j], sum[i][j]);
-        __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int64_t n = i0 + ti + i;
-            const int m = j0 + tj + j;
-            if (n >= I || m >= J) continue;
-            const float z = sum[i][j] + (e.bias ? e.bias[m] : 0.f);
-            if (e.Z) static_cast<T*>(e.Z)[n * e.ldz + m] = (T)z;
-            const float r = e.R ? (float)static_cast<const T*>(e.R)[n * e.ldr + m] : 0.f;
-            static_cast<T*>(e.Y)[n * e.ldy + m] = (T)(activate(z, e.activation) + r);
-        }
-}
-
-template <class T>
-hipError_t product(const T* A, int64_t ai, int64_t ak, const T* B, int64_t bk, int64_t bj, int64_t I, int J, int64_t K,
-                   const Epilogue& e, hipStream_t s) {
-    const int64_t j_tiles = (J + kTile - 1) / kTile, blocks = j_tiles * ((I + kTile - 1) / kTile);
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(product_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, A, ai, ak, B, bk, bj, I, J, K, (int)j_tiles, e);
-    return hipGetLastError();
-}
-
-// dZ = G act'(Z)
-template <class T>
-__global__ __launch_bounds__(256) void slope_kernel(const T* __restrict__ G, int64_t ldg, const T* __restrict__ Z, int64_t ldz,
-                                                    int64_t N, int M, int activation, T* __restrict__ dZ) {
-    for (int64_t v = blockIdx.x * 256LL + threadIdx.x; v < N * M; v += gridDim.x * 256LL) {
-        const int64_t n = v / M;
-        const int m = (int)(v - n * M);
-        dZ[v] = (T)((float)G[n * ldg + m] * slope((float)Z[n * ldz + m], activation));
+__global__ __launch_bounds__(256) void lay_out_kernel(LayOut a) {
+    int64_t units[2];
+    for (int m = 0; m < 2; ++m) units[m] = a.to[m] ? a.rows[m] * (laid_out_units(a.width[m])) : 0;
+    for (int64_t v = blockIdx.x * 256LL + threadIdx.x; v < units[0] + units[1]; v += gridDim.x * 256LL) {
+        const int m = v >= units[0];
+        const int64_t u = m ? v - units[0] : v, per_row = laid_out_units(a.width[m]);
+        const int64_t row = u / per_row, col = (u - row * per_row) * kVec;
+        float x[kVec];
+        load_row(static_cast<const T*>(a.from[m]) + row * a.ld[m], col, a.width[m], x);
+        lay_out<T>(x, a.to[m] + u * kVec, a.rows[m] * per_row * kVec);
     }
 }
 
-// grid: columns / 32
+struct SlopeArgs {
+    const void *G, *Z;
+    int64_t ldg, ldz, N;
+    int M, activation;
+    uint16_t* to;    // dZ laid out; may be missing
+    float* partial;  // [row chunks][M] sums of dZ's columns; may be missing
+    int lanes, col_tiles, chunks;
+};
+
+// dZ = G act'(Z), laid out, and its column sums.  A workgroup takes 8 * lanes columns and every chunks-th group of rows; a thread
+// keeps its eight columns.  grid: chunks * col_tiles, column tile fastest.
 template <class T>
-__global__ __launch_bounds__(256) void bias_sums_kernel(const T* __restrict__ G, int64_t ldg, const T* __restrict__ Z, int64_t ldz,
-                                                        int64_t N, int M, int activation, float* __restrict__ db) {
-    __shared__ double part[8][32];
-    const int i = threadIdx.x & 31, group = threadIdx.x >> 5, m = blockIdx.x * 32 + i;
-    double sum = 0;
-    if (m < M)
-        for (int64_t n = group; n < N; n += 8)
-            sum += (float)G[n * ldg + m] * (activation ? slope((float)Z[n * ldz + m], activation) : 1.f);
-    part[group][i] = sum;
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
+    __shared__ float part[256][kVec + 1];
+    const int sub = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes, rows = 256 / a.lanes;
+    const int64_t col = ((int64_t)(blockIdx.x % a.col_tiles) * a.lanes + lane) * kVec;
+    const int chunk = blockIdx.x / a.col_tiles;
+    const int64_t ldt = round8(a.M);
+    float sum[kVec] = {};
+    if (col < a.M) {
+        for (int64_t n = (int64_t)chunk * rows + sub; n < a.N; n += (int64_t)a.chunks * rows) {
+            float g[kVec];
+            load_row(static_cast<const T*>(a.G) + n * a.ldg, col, a.M, g);
+            if (a.activation) {
+                float z[kVec];
+                load_row(static_cast<const T*>(a.Z) + n * a.ldz, col, a.M, z);
+                slope_all(g, z, a.activation);
+            }
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) sum[i] += g[i];
+            if (a.to) lay_out<T>(g, a.to + n * ldt + col, a.N * ldt);
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) part[threadIdx.x][i] = sum[i];
     __syncthreads();
-    if (group != 0 || m >= M) return;
-    for (int k = 1; k < 8; ++k) sum += part[k][i];
-    db[m] = (float)sum;
+    for (int v = threadIdx.x; v < a.lanes * kVec; v += 256) {
+        const int64_t m = (int64_t)(blockIdx.x % a.col_tiles) * a.lanes * kVec + v;
+        float total = 0.f;
+        for (int r = 0; r < rows; ++r) total += part[r * a.lanes + v / kVec][v % kVec];
+        if (m < a.M) a.partial[(int64_t)chunk * a.M + m] = total;
+    }
 }
 
-}  // namespace
+// How the rows are shared out: a power of two of lanes per row, and eight rows per thread or 4 workgroups per compute unit.
+void share_rows(int64_t N, int M, SlopeArgs& a) {
+    a.lanes = 1;
+    while (a.lanes < 64 && a.lanes * kVec < M) a.lanes *= 2;
+    a.col_tiles = (int)((M + a.lanes * kVec - 1) / (a.lanes * kVec));
+    const int64_t per_chunk = 256 / a.lanes * 8;
+    a.chunks = (int)std::max<int64_t>(1, std::min<int64_t>((N + per_chunk - 1) / per_chunk, std::max(4 * compute_units() / a.col_tiles, 1)));
+}
 
-size_t dense_linear_workspace(const DenseCall&) { return 0; }
+// dW and db of no rows
+template <class T>
+__global__ __launch_bounds__(256) void clear_kernel(T* dW, int64_t ld, int64_t rows, int M, float* db) {
+    for (int64_t v = blockIdx.x * 256LL + threadIdx.x; v < (rows + 1) * M; v += gridDim.x * 256LL) {
+        const int64_t row = v / M, m = v - row * M;
+        if (row < rows) {
+            if (dW) dW[row * ld + m] = (T)0.f;
+        } else if (db) {
+            db[m] = 0.f;
+        }
+    }
+}
 
-hipError_t launch_dense_linear(const DenseCall& c, const float* bias, int activation, const void* R, int64_t ldr, void* Y,
-                               int64_t ldy, void* Z, int64_t ldz, void*, hipStream_t s) {
-    return with_type(c.dtype, [&](auto t) {
+hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db, hipStream_t s) {
+    if (!dW && !db) return hipSuccess;
+    return with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        return product(static_cast<const T*>(c.X), c.ldx, 1, static_cast<const T*>(c.W), c.ldw, 1, c.N, c.M, c.D,
-                       Epilogue{bias, activation, R, Y, Z, ldr, ldy, ldz}, s);
+        hipLaunchKernelGGL(clear_kernel<T>, dim3(1024), dim3(256), 0, s, static_cast<T*>(dW), ld, (int64_t)D, M, db);
+        return hipGetLastError();
     });
 }
 
-size_t dense_linear_gradient_workspace(const DenseCall& c, const void*, int64_t, const void*, int64_t, int activation, bool, bool, bool) {
-    return activation ? (size_t)c.N * c.M * (c.dtype ? 2 : 4) : 0;
+// A product's tile and how many workgroups share a tile's sum.
+struct Plan {
+    int tile, splits;
+};
+struct TileSize {
+    int i, j, depth;
+};
+constexpr TileSize kTiles16[] = {{256, 256, 64}, {128, 128, 64}, {64, 64, 64}}, kTilesF32[] = {{128, 128, 32}, {64, 64, 32}};
+
+Plan plan(int dtype, int64_t I, int J, int64_t K) {
+    const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
+    const int count = dtype == 0 ? 2 : 3;
+    const auto tiles = [&](int t) { return ((I + sizes[t].i - 1) / sizes[t].i) * ((J + sizes[t].j - 1) / sizes[t].j); };
+    int t = 0;
+    while (t + 1 < count && tiles(t) < compute_units() * 3 / 4) ++t;
+    const int64_t k_tiles = (K + sizes[t].depth - 1) / sizes[t].depth;
+    const int64_t splits = std::min<int64_t>(std::max<int64_t>(compute_units() / tiles(t), 1), std::max<int64_t>(k_tiles / 4, 1));
+    return {t, (int)std::min<int64_t>(splits, 64)};
+}
+
+size_t partial_bytes(const Plan& p, int64_t I, int J) { return p.splits > 1 ? (size_t)round_up((int64_t)p.splits * I * J * 4, 256) : 0; }
+
+hipError_t run(int dtype, const Plan& p, bool a_k, bool b_k, const Operand& A, const Operand& B, int64_t I, int J, int64_t K, void* partial,
+               const Epilogue& e, hipStream_t s) {
+    ProductArgs a = {A, B, I, K, J, 0, 0, p.splits, static_cast<float*>(partial), e};
+    switch (dtype) {
+        case 0: return launch_product_f32(p.tile, a_k, b_k, a, s);
+        case 1: return launch_product_bf16(p.tile, a_k, b_k, a, s);
+        default: return launch_product_f16(p.tile, a_k, b_k, a, s);
+    }
+}
+
+hipError_t lay_out_matrices(int dtype, const LayOut& a, hipStream_t s) {
+    int64_t units = 0;
+    for (int m = 0; m < 2; ++m)
+        if (a.to[m]) units += a.rows[m] * (laid_out_stride(a.width[m]) / kVec);
+    if (units == 0) return hipSuccess;
+    return with_type(dtype, [&](auto t) {
+        hipLaunchKernelGGL(lay_out_kernel<decltype(t)>, dim3((unsigned)std::min<int64_t>((units + 255) / 256, 1 << 15)), dim3(256), 0, s, a);
+        return hipGetLastError();
+    });
+}
+
+// Shares of the workspace, in the order that they are asked for.
+struct Shares {
+    char* at;
+    void* take(size_t bytes) {
+        char* const p = at;
+        at += bytes;
+        return p;
+    }
+};
+
+// A matrix of the call as an operand: itself, or where it is laid out.  k_inner: its rows run along k.
+Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t rows, int64_t width, bool k_inner, bool f32) {
+    const float* const origin = f32 ? static_cast<const float*>(given) : nullptr;
+    Operand o = {given, ld, 0, origin, k_inner ? ld : 1, k_inner ? 1 : ld, nullptr, 0, 0, 0};
+    if (laid_out) o.p = laid_out, o.ld = laid_out_stride(width), o.plane = rows * o.ld;
+    return o;
+}
+
+// What the backward pass has to have laid out, and its products.
+struct GradientPlan {
+    bool x, w, z, sums, pass;
+    Plan to_x, to_w;
+    SlopeArgs slope;
+    size_t partial;
+};
+
+GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int activation, bool need_dx, bool need_dw, bool need_db) {
+    GradientPlan g = {};
+    g.x = need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
+    g.w = need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
+    g.z = (need_dx || need_dw) && (activation != 0 || !usable(c.dtype, G, ldg, c.M));
+    g.sums = need_db;
+    g.pass = g.z || g.sums;
+    if (need_dx) g.to_x = plan(c.dtype, c.N, c.D, c.M);
+    if (need_dw) g.to_w = plan(c.dtype, c.D, c.M, c.N);
+    share_rows(c.N, c.M, g.slope);
+    g.partial = std::max(need_dx ? partial_bytes(g.to_x, c.N, c.D) : 0, need_dw ? partial_bytes(g.to_w, c.D, c.M) : 0);
+    return g;
+}
+
+size_t column_bytes(const GradientPlan& g, int M) { return g.sums ? (size_t)round_up((int64_t)g.slope.chunks * M * 4, 256) : 0; }
+
+}  // namespace
+
+size_t dense_linear_workspace(const DenseCall& c) {
+    return (usable(c.dtype, c.X, c.ldx, c.D) ? 0 : laid_out_bytes(c.dtype, c.N, c.D)) +
+           (usable(c.dtype, c.W, c.ldw, c.M) ? 0 : laid_out_bytes(c.dtype, c.D, c.M)) + partial_bytes(plan(c.dtype, c.N, c.M, c.D), c.N, c.M);
+}
+
+hipError_t launch_dense_linear(const DenseCall& c, const float* bias, int activation, const void* R, int64_t ldr, void* Y,
+                               int64_t ldy, void* Z, int64_t ldz, void* workspace, hipStream_t s) {
+    Shares shares = {static_cast<char*>(workspace)};
+    const Plan p = plan(c.dtype, c.N, c.M, c.D);
+    uint16_t *x = nullptr, *w = nullptr;
+    if (!usable(c.dtype, c.X, c.ldx, c.D)) x = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.D)));
+    if (!usable(c.dtype, c.W, c.ldw, c.M)) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
+    if (hipError_t e = lay_out_matrices(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
+    const bool f32 = c.dtype == 0;
+    return run(c.dtype, p, true, false, operand(c.X, c.ldx, x, c.N, c.D, true, f32), operand(c.W, c.ldw, w, c.D, c.M, false, f32), c.N, c.M,
+               c.D, shares.take(0), {bias, activation, R, Y, Z, ldr, ldy, ldz}, s);
+}
+
+size_t dense_linear_gradient_workspace(const DenseCall& c, const void* G, int64_t ldg, const void*, int64_t, int activation,
+                                       bool need_dx, bool need_dw, bool need_db) {
+    const GradientPlan g = gradient_plan(c, G, ldg, activation, need_dx, need_dw, need_db);
+    return (g.x ? laid_out_bytes(c.dtype, c.N, c.D) : 0) + (g.w ? laid_out_bytes(c.dtype, c.D, c.M) : 0) +
+           (g.z ? laid_out_bytes(c.dtype, c.N, c.M) : 0) + column_bytes(g, c.M) + g.partial;
 }
 
 hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64_t ldg, const void* Z, int64_t ldz, int activation,
                                         void* dX, int64_t lddx, void* dW, int64_t lddw, float* db, void* workspace,
                                         hipStream_t s) {
-    return with_type(c.dtype, [&](auto t) {
-        using T = decltype(t);
-        const T *g = static_cast<const T*>(G), *z = static_cast<const T*>(Z);
+    if (c.N == 0) return launch_clear(c.dtype, dW, lddw, c.D, c.M, db, s);
+    GradientPlan g = gradient_plan(c, G, ldg, activation, dX, dW, db);
+    Shares shares = {static_cast<char*>(workspace)};
+    uint16_t *x = nullptr, *w = nullptr, *z = nullptr;
+    if (g.x) x = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.D)));
+    if (g.w) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
+    if (g.z) z = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.M)));
+    float* const columns = static_cast<float*>(shares.take(column_bytes(g, c.M)));
+    if (hipError_t e = lay_out_matrices(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
+    if (g.pass) {
+        SlopeArgs& a = g.slope;
+        a.G = G, a.Z = Z, a.ldg = ldg, a.ldz = ldz, a.N = c.N, a.M = c.M, a.activation = activation;
+        a.to = z, a.partial = db ? columns : nullptr;
+        const hipError_t e = with_type(c.dtype, [&](auto t) {
+            hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles)), dim3(256), 0, s, a);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
         if (db)
-            hipLaunchKernelGGL(bias_sums_kernel<T>, dim3((c.M + 31) / 32), dim3(256), 0, s, g, ldg, z, ldz, c.N, c.M, activation, db);
-        if (activation && (dX || dW) && c.N > 0) {
-            T* const dz = static_cast<T*>(workspace);
-            hipLaunchKernelGGL(slope_kernel<T>, dim3(2048), dim3(256), 0, s, g, ldg, z, ldz, c.N, c.M, activation, dz);
-            g = dz;
-            ldg = c.M;
+            if (hipError_t e = launch_partial_sums(columns, a.chunks, c.M, c.M, db, nullptr, s)) return e;
+    }
+    const bool f32 = c.dtype == 0;
+    const auto gradient = [&](bool k_inner) {
+        Operand o = operand(G, ldg, z, c.N, c.M, k_inner, f32);
+        if (f32 && activation) {
+            o.slope_of = static_cast<const float*>(Z), o.activation = activation;
+            o.slope_outer = k_inner ? ldz : 1, o.slope_k = k_inner ? 1 : ldz;
         }
-        if (hipError_t e = hipGetLastError()) return e;
-        const Epilogue to_x{nullptr, 0, nullptr, dX, nullptr, 0, lddx, 0}, to_w{nullptr, 0, nullptr, dW, nullptr, 0, lddw, 0};
-        if (dX && c.N > 0)
-            if (hipError_t e = product(g, ldg, 1, static_cast<const T*>(c.W), 1, c.ldw, c.N, c.D, c.M, to_x, s)) return e;
-        if (!dW) return hipSuccess;
-        return product(static_cast<const T*>(c.X), 1, c.ldx, g, ldg, 1, c.D, c.M, c.N, to_w, s);
-    });
+        return o;
+    };
+    void* const partial = shares.take(0);
+    if (dX)
+        if (hipError_t e = run(c.dtype, g.to_x, true, true, gradient(true), operand(c.W, c.ldw, w, c.D, c.M, true, f32), c.N, c.D, c.M,
+                               partial, {nullptr, 0, nullptr, dX, nullptr, 0, lddx, 0}, s))
+            return e;
+    if (!dW) return hipSuccess;
+    return run(c.dtype, g.to_w, false, false, operand(c.X, c.ldx, x, c.N, c.D, false, f32), gradient(false), c.D, c.M, c.N, partial,
+               {nullptr, 0, nullptr, dW, nullptr, 0, lddw, 0}, s);
 }
 
 }  // namespace lutnn

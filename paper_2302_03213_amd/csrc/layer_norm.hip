@@ -222,24 +222,6 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
     leave(db, mine + a.D);
 }
 
-// out[d] = sum over the workgroups of partial[workgroup][d], for the 2 D columns of both gradients: 32 columns per workgroup, every
-// eighth partial sum per thread, 64-bit sums in a fixed order.
-__global__ __launch_bounds__(256) void norm_column_sums_kernel(const float* __restrict__ partial, int count, int D,
-                                                               float* __restrict__ dw, float* __restrict__ db) {
-    __shared__ double part[8][32];
-    const int i = threadIdx.x & 31, group = threadIdx.x >> 5, d = blockIdx.x * 32 + i;
-    double sum = 0;
-    if (d < 2 * D)
-        for (int k = group; k < count; k += 8) sum += partial[(int64_t)k * 2 * D + d];
-    part[group][i] = sum;
-    __syncthreads();
-    if (group != 0 || d >= 2 * D) return;
-#pragma unroll
-    for (int k = 1; k < 8; ++k) sum += part[k][i];
-    float* const out = d < D ? dw : db;
-    if (out) out[d < D ? d : d - D] = (float)sum;
-}
-
 template <class T, class F>
 hipError_t by_width(int D, F&& f) {
     using std::integral_constant;
@@ -300,9 +282,7 @@ hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64
         if (e != hipSuccess) return e;
     }
     if (!dw && !db) return hipSuccess;
-    hipLaunchKernelGGL(norm_column_sums_kernel, dim3((unsigned)((2 * D + 31) / 32)), dim3(256), 0, s,
-                       static_cast<const float*>(workspace), groups, D, dw, db);
-    return hipGetLastError();
+    return launch_partial_sums(static_cast<const float*>(workspace), groups, 2 * D, D, dw, db, s);
 }
 
 }  // namespace lutnn

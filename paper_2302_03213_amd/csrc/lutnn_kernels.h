@@ -110,6 +110,10 @@ hipError_t launch_matmul_split(const float* G, int64_t N, int64_t ldg, const flo
 size_t column_sums_workspace(int64_t outer, int M, int64_t inner);
 hipError_t launch_column_sums(const float* G, int64_t outer, int64_t ldg, int M, int64_t inner, void* workspace, float* out,
                               hipStream_t s);
+// fp32 sums that a kernel's workgroups left, [count][width], added up: the first `first` columns to `out`, the others to `rest`
+// (either may be missing).
+hipError_t launch_partial_sums(const float* partial, int count, int64_t width, int64_t first, float* out, float* rest,
+                               hipStream_t s);
 
 // Z[b][d][l] = sum_m W[d][m] G[b][m][l]: the im2col gradient of the ordinary convolution with weights W.
 hipError_t launch_conv_z(const float* W, int64_t ldw, const float* G, int64_t B, int D, int M, const ConvGeom& g, float* Z,
