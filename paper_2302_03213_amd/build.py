@@ -23,7 +23,7 @@ TORCH_CALLS = os.path.join(PKG, "torch_calls.so")  # csrc/torch_calls.cpp: host 
 
 SOURCES = ["api.hip", "encode.hip", "encode_conv9.hip", "encode_tree.hip", "build_table.hip", "lookup_lds.hip", "lookup_rows.hip", "lookup_mfma.hip", "lookup_smfmac.hip", "lookup_wide.hip", "lookup_matrix_f32.hip",
            "linear_fused.hip", "linear_small.hip", "softpq_backward.hip", "softpq_matrix.hip", "softpq_conv.hip", "matmul_split.hip", "column_sums.hip",
-           "dense_linear.hip", "dense_product_f32.hip", "dense_product_bf16.hip", "dense_product_f16.hip", "layer_norm.hip", "probe_smfmac.hip"]
+           "dense_linear.hip", "dense_rows.hip", "dense_product_f32.hip", "dense_product_bf16.hip", "dense_product_f16.hip", "layer_norm.hip", "probe_smfmac.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "dense_product.h"
+#include "dense_rows.h"
 
 namespace lutnn {
 namespace {
@@ -86,6 +87,7 @@ struct SlopeArgs {
     int64_t ldg, ldz, N;
     int M, activation;
     uint16_t* to;    // dZ laid out; may be missing
+    bool plain;      // ... or, of fp32, as it is
     float* partial;  // [row chunks][M] sums of dZ's columns; may be missing
     int lanes, col_tiles, chunks;
 };
@@ -111,7 +113,14 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
             }
 #pragma unroll
             for (int i = 0; i < kVec; ++i) sum[i] += g[i];
-            if (a.to) lay_out<T>(g, a.to + n * ldt + col, a.N * ldt);
+            if (a.to && a.plain) {
+                float* const at = reinterpret_cast<float*>(a.to) + n * a.M + col;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i)
+                    if (col + i < a.M) at[i] = g[i];
+            } else if (a.to) {
+                lay_out<T>(g, a.to + n * ldt + col, a.N * ldt);
+            }
         }
     }
     if (!a.partial) return;
@@ -157,31 +166,77 @@ hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db
     });
 }
 
-// A product's tile and how many workgroups share a tile's sum.
-struct Plan {
-    int tile, splits;
-};
+// The tiles of launch_tile (dense_product.h), how many of them a compute unit holds, and what 1 .. that many at once take, in us: per
+// 64 k, and beside that.  From products of 16 x 16 n tiles at K = 512 and 2560, the three layouts' average.  Small tiles are bound by
+// what a compute unit gets from L2 (75 GB/s), the large ones by the matrix instructions and the power they draw.
 struct TileSize {
-    int i, j, depth;
+    int i, j, depth, at_once;
+    float stage[4], rest[4];
 };
-constexpr TileSize kTiles16[] = {{256, 256, 64}, {128, 128, 64}, {64, 64, 64}}, kTilesF32[] = {{128, 128, 32}, {64, 64, 32}};
+constexpr TileSize kTiles16[] = {{256, 256, 32, 1, {1.55f}, {9.0f}},
+                                 {128, 128, 64, 2, {0.78f, 0.90f}, {2.0f, 5.0f}},
+                                 {64, 128, 64, 2, {0.61f, 0.65f}, {0.5f, 2.5f}},
+                                 {64, 64, 64, 3, {0.23f, 0.46f, 0.66f}, {1.0f, 0.7f, 1.0f}},
+                                 {32, 64, 64, 4, {0.16f, 0.37f, 0.56f, 0.72f}, {1.0f, 0.5f, 0.5f, 0.5f}}};
+constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {4.2f}, {12.0f}},
+                                  {128, 128, 32, 1, {2.4f}, {4.5f}},
+                                  {64, 128, 32, 2, {2.0f, 2.6f}, {0.5f, 5.5f}},
+                                  {64, 64, 32, 3, {1.4f, 1.65f, 2.4f}, {0.0f, 1.5f, 4.0f}}};
+constexpr float kLaunchUs = 2.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
 
-Plan plan(int dtype, int64_t I, int J, int64_t K) {
-    const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
-    const int count = dtype == 0 ? 2 : 3;
-    const auto tiles = [&](int t) { return ((I + sizes[t].i - 1) / sizes[t].i) * ((J + sizes[t].j - 1) / sizes[t].j); };
-    int t = 0;
-    while (t + 1 < count && tiles(t) < compute_units() * 3 / 4) ++t;
-    const int64_t k_tiles = (K + sizes[t].depth - 1) / sizes[t].depth;
-    const int64_t splits = std::min<int64_t>(std::max<int64_t>(compute_units() / tiles(t), 1), std::max<int64_t>(k_tiles / 4, 1));
-    return {t, (int)std::min<int64_t>(splits, 64)};
+// A product's tile, how many of its tiles are one workgroup's, and how many workgroups share the sum of each of the others.
+struct Plan {
+    int tile, whole, splits;
+    int64_t tiles;
+    float us;
+};
+
+float tiles_us(const TileSize& t, int64_t count, float stages) {
+    const int64_t units = compute_units(), rounds = count / (units * t.at_once), rest = count - rounds * units * t.at_once;
+    float us = rounds * (stages * t.stage[t.at_once - 1] + t.rest[t.at_once - 1]);
+    if (rest > 0) {
+        const int n = (int)((rest + units - 1) / units) - 1;
+        us += stages * t.stage[n] + t.rest[n];
+    }
+    return us;
 }
 
-size_t partial_bytes(const Plan& p, int64_t I, int J) { return p.splits > 1 ? (size_t)round_up((int64_t)p.splits * I * J * 4, 256) : 0; }
+// The fastest by those figures.  A sum is shared out where the last tiles would leave most of the chip idle for longer than a second
+// launch, which adds up what the first left in memory, takes.
+Plan plan(int dtype, int64_t I, int J, int64_t K) {
+    const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
+    const int count = dtype == 0 ? 4 : 5;
+    Plan best = {0, 0, 1, 0, 1e30f};
+    for (int i = 0; i < count; ++i) {
+        const TileSize& t = sizes[i];
+        const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
+        const float stage = t.depth / 64.f;
+        const float us = kLaunchUs + tiles_us(t, tiles, k_tiles * stage);
+        if (us < best.us) best = {i, (int)std::min<int64_t>(tiles, 1 << 30), 1, tiles, us};
+        const int64_t slots = compute_units() * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
+        const float base = kLaunchUs + kJoinUs + tiles_us(t, whole, k_tiles * stage);
+        if (shared == 0 || base >= best.us) continue;
+        for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (splits > k_tiles) break;
+            const float bytes = 2.f * splits * shared * t.i * t.j * 4;
+            const float shared_us = base + tiles_us(t, shared * splits, (float)((k_tiles + splits - 1) / splits) * stage) + bytes / kBytesPerUs;
+            if (shared_us < best.us) best = {i, (int)whole, splits, tiles, shared_us};
+        }
+    }
+    return best;
+}
+
+size_t partial_bytes(int dtype, const Plan& p) {
+    const TileSize& t = dtype == 0 ? kTilesF32[p.tile] : kTiles16[p.tile];
+    return p.splits > 1 ? (size_t)p.splits * (p.tiles - p.whole) * t.i * t.j * 4 : 0;
+}
+
+// Laying `values` fp32 values out: read, and written as three parts.
+float lay_out_us(float values) { return kLaunchUs + values * 10 / kBytesPerUs; }
 
 hipError_t run(int dtype, const Plan& p, bool a_k, bool b_k, const Operand& A, const Operand& B, int64_t I, int J, int64_t K, void* partial,
                const Epilogue& e, hipStream_t s) {
-    ProductArgs a = {A, B, I, K, J, 0, 0, p.splits, static_cast<float*>(partial), e};
+    ProductArgs a = {A, B, I, K, J, 0, 0, p.whole, p.splits, static_cast<float*>(partial), e};
     switch (dtype) {
         case 0: return launch_product_f32(p.tile, a_k, b_k, a, s);
         case 1: return launch_product_bf16(p.tile, a_k, b_k, a, s);
@@ -220,6 +275,7 @@ Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t
 
 // What the backward pass has to have laid out, and its products.
 struct GradientPlan {
+    bool plain;  // fp32 products of the operands as they are
     bool x, w, z, sums, pass;
     Plan to_x, to_w;
     SlopeArgs slope;
@@ -228,45 +284,83 @@ struct GradientPlan {
 
 GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int activation, bool need_dx, bool need_dw, bool need_db) {
     GradientPlan g = {};
-    g.x = need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
-    g.w = need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
-    g.z = (need_dx || need_dw) && (activation != 0 || !usable(c.dtype, G, ldg, c.M));
+    float tiles = 0.f, plain = 0.f, values = (float)c.N * c.M;
+    if (need_dx) {
+        g.to_x = plan(c.dtype, c.N, c.D, c.M);
+        tiles += g.to_x.us, plain += plain_f32_us(c.N, c.D, c.M), values += (float)c.D * c.M;
+    }
+    if (need_dw) {
+        g.to_w = plan(c.dtype, c.D, c.M, c.N);
+        tiles += g.to_w.us, plain += plain_f32_us(c.D, c.M, c.N), values += (float)c.N * c.D;
+    }
+    g.plain = c.dtype == 0 && plain < tiles + lay_out_us(values);
+    g.x = !g.plain && need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
+    g.w = !g.plain && need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
+    g.z = (need_dx || need_dw) && (activation != 0 || (!g.plain && !usable(c.dtype, G, ldg, c.M)));
     g.sums = need_db;
     g.pass = g.z || g.sums;
-    if (need_dx) g.to_x = plan(c.dtype, c.N, c.D, c.M);
-    if (need_dw) g.to_w = plan(c.dtype, c.D, c.M, c.N);
     share_rows(c.N, c.M, g.slope);
-    g.partial = std::max(need_dx ? partial_bytes(g.to_x, c.N, c.D) : 0, need_dw ? partial_bytes(g.to_w, c.D, c.M) : 0);
+    if (!g.plain) g.partial = std::max(need_dx ? partial_bytes(c.dtype, g.to_x) : 0, need_dw ? partial_bytes(c.dtype, g.to_w) : 0);
     return g;
 }
 
+size_t slope_bytes(const DenseCall& c, const GradientPlan& g) {
+    return g.plain ? (size_t)round_up(c.N * c.M * 4, 256) : laid_out_bytes(c.dtype, c.N, c.M);
+}
 size_t column_bytes(const GradientPlan& g, int M) { return g.sums ? (size_t)round_up((int64_t)g.slope.chunks * M * 4, 256) : 0; }
 
 }  // namespace
 
+namespace {
+
+// How a forward pass goes: few rows, plain fp32, or tiles of operands that may have to be laid out.
+struct ForwardPlan {
+    bool few, plain, x, w;
+    Plan product;
+};
+
+ForwardPlan forward_plan(const DenseCall& c) {
+    ForwardPlan f = {};
+    f.few = c.N <= kFewRows;
+    if (f.few) return f;
+    f.product = plan(c.dtype, c.N, c.M, c.D);
+    f.plain = c.dtype == 0 && plain_f32_us(c.N, c.M, c.D) < f.product.us + lay_out_us((float)c.N * c.D + (float)c.D * c.M);
+    f.x = !f.plain && !usable(c.dtype, c.X, c.ldx, c.D);
+    f.w = !f.plain && !usable(c.dtype, c.W, c.ldw, c.M);
+    return f;
+}
+
+}  // namespace
+
 size_t dense_linear_workspace(const DenseCall& c) {
-    return (usable(c.dtype, c.X, c.ldx, c.D) ? 0 : laid_out_bytes(c.dtype, c.N, c.D)) +
-           (usable(c.dtype, c.W, c.ldw, c.M) ? 0 : laid_out_bytes(c.dtype, c.D, c.M)) + partial_bytes(plan(c.dtype, c.N, c.M, c.D), c.N, c.M);
+    const ForwardPlan f = forward_plan(c);
+    if (f.few || f.plain) return 0;
+    return (f.x ? laid_out_bytes(c.dtype, c.N, c.D) : 0) + (f.w ? laid_out_bytes(c.dtype, c.D, c.M) : 0) + partial_bytes(c.dtype, f.product);
 }
 
 hipError_t launch_dense_linear(const DenseCall& c, const float* bias, int activation, const void* R, int64_t ldr, void* Y,
                                int64_t ldy, void* Z, int64_t ldz, void* workspace, hipStream_t s) {
+    const ForwardPlan f = forward_plan(c);
+    const Epilogue epilogue = {bias, activation, R, Y, Z, ldr, ldy, ldz};
+    if (f.few) return launch_few_rows(c.dtype, c.X, c.N, c.ldx, c.W, c.ldw, c.D, c.M, epilogue, s);
+    if (f.plain)
+        return launch_plain_f32({static_cast<const float*>(c.X), c.ldx, 1}, {static_cast<const float*>(c.W), 1, c.ldw}, c.N, c.M, c.D,
+                                epilogue, s);
     Shares shares = {static_cast<char*>(workspace)};
-    const Plan p = plan(c.dtype, c.N, c.M, c.D);
     uint16_t *x = nullptr, *w = nullptr;
-    if (!usable(c.dtype, c.X, c.ldx, c.D)) x = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.D)));
-    if (!usable(c.dtype, c.W, c.ldw, c.M)) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
+    if (f.x) x = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.D)));
+    if (f.w) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
     if (hipError_t e = lay_out_matrices(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
     const bool f32 = c.dtype == 0;
-    return run(c.dtype, p, true, false, operand(c.X, c.ldx, x, c.N, c.D, true, f32), operand(c.W, c.ldw, w, c.D, c.M, false, f32), c.N, c.M,
-               c.D, shares.take(0), {bias, activation, R, Y, Z, ldr, ldy, ldz}, s);
+    return run(c.dtype, f.product, true, false, operand(c.X, c.ldx, x, c.N, c.D, true, f32), operand(c.W, c.ldw, w, c.D, c.M, false, f32),
+               c.N, c.M, c.D, shares.take(0), epilogue, s);
 }
 
 size_t dense_linear_gradient_workspace(const DenseCall& c, const void* G, int64_t ldg, const void*, int64_t, int activation,
                                        bool need_dx, bool need_dw, bool need_db) {
     const GradientPlan g = gradient_plan(c, G, ldg, activation, need_dx, need_dw, need_db);
     return (g.x ? laid_out_bytes(c.dtype, c.N, c.D) : 0) + (g.w ? laid_out_bytes(c.dtype, c.D, c.M) : 0) +
-           (g.z ? laid_out_bytes(c.dtype, c.N, c.M) : 0) + column_bytes(g, c.M) + g.partial;
+           (g.z ? slope_bytes(c, g) : 0) + column_bytes(g, c.M) + g.partial;
 }
 
 hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64_t ldg, const void* Z, int64_t ldz, int activation,
@@ -278,13 +372,13 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     uint16_t *x = nullptr, *w = nullptr, *z = nullptr;
     if (g.x) x = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.D)));
     if (g.w) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
-    if (g.z) z = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.M)));
+    if (g.z) z = static_cast<uint16_t*>(shares.take(slope_bytes(c, g)));
     float* const columns = static_cast<float*>(shares.take(column_bytes(g, c.M)));
     if (hipError_t e = lay_out_matrices(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
     if (g.pass) {
         SlopeArgs& a = g.slope;
         a.G = G, a.Z = Z, a.ldg = ldg, a.ldz = ldz, a.N = c.N, a.M = c.M, a.activation = activation;
-        a.to = z, a.partial = db ? columns : nullptr;
+        a.to = z, a.plain = g.plain, a.partial = db ? columns : nullptr;
         const hipError_t e = with_type(c.dtype, [&](auto t) {
             hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles)), dim3(256), 0, s, a);
             return hipGetLastError();
@@ -292,6 +386,16 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
         if (e != hipSuccess) return e;
         if (db)
             if (hipError_t e = launch_partial_sums(columns, a.chunks, c.M, c.M, db, nullptr, s)) return e;
+    }
+    if (g.plain) {
+        const float *const dz = static_cast<const float*>(g.z ? static_cast<const void*>(z) : G), *const X = static_cast<const float*>(c.X);
+        const int64_t ld = g.z ? c.M : ldg;
+        if (dX)
+            if (hipError_t e = launch_plain_f32({dz, ld, 1}, {static_cast<const float*>(c.W), c.ldw, 1}, c.N, c.D, c.M,
+                                                {nullptr, 0, nullptr, dX, nullptr, 0, lddx, 0}, s))
+                return e;
+        return !dW ? hipSuccess
+                   : launch_plain_f32({X, 1, c.ldx}, {dz, 1, ld}, c.D, c.M, c.N, {nullptr, 0, nullptr, dW, nullptr, 0, lddw, 0}, s);
     }
     const bool f32 = c.dtype == 0;
     const auto gradient = [&](bool k_inner) {

@@ -3,23 +3,12 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "activation.h"
+#include "dense_epilogue.h"
 #include "lutnn_kernels.h"
-#include "matrix_types.h"
 #include "mfma_tile.h"
 #include "split_bf16.h"
 
 namespace lutnn {
-
-// What becomes of a sum: bias, activation and residual; Z receives it before the activation.
-struct Epilogue {
-    const float* bias;
-    int activation;
-    const void* R;
-    void* Y;
-    void* Z;
-    int64_t ldr, ldy, ldz;
-};
 
 // An operand as the kernel reads it: 16-bit values, rows of `ld` of them in whole aligned 16-byte units, zeros behind a row's end as
 // far as its unit goes; PARTS planes.
@@ -38,14 +27,16 @@ struct Operand {
 struct ProductArgs {
     Operand A, B;
     int64_t I, K;
-    int J, i_tiles, j_tiles, splits;
-    float* partial;  // [splits][I][J] where splits > 1
+    int J, i_tiles, j_tiles;
+    int whole, splits;  // so many tiles are one workgroup's each; `splits` share the sum of each of the others
+    float* partial;     // theirs: [splits][tiles - whole][rows of a tile][columns of it]
     Epilogue e;
 };
 
 namespace product {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -60,6 +51,13 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c, bf16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c, f16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
 // Orders the workgroup's LDS operations only: loads to LDS stay in flight.
 __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -67,7 +65,8 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// 64 lanes x 16 bytes from the buffer `rsrc` straight into LDS at lds_dst + 16 * lane; zeros for offsets past its end.
+// 64 lanes x 16 bytes from the buffer `rsrc` straight into LDS at lds_dst + 16 * lane; zeros for offsets past its end.  Nothing
+// is said of LDS being written: reads of other buffers may move across, and wait_loads keeps those of this one behind it.
 __device__ __forceinline__ void buffer_to_lds(uint32_t lds_dst, i32x4 rsrc, uint32_t voff) {
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
@@ -75,7 +74,7 @@ __device__ __forceinline__ void buffer_to_lds(uint32_t lds_dst, i32x4 rsrc, uint
         "buffer_load_dwordx4 %1, %2, 0 offen lds"
         :
         : "s"(lds_dst), "v"(voff), "s"(rsrc)
-        : "memory", "m0");
+        : "m0");
 }
 
 // One operand's tile: `OUT` rows (of A) or columns (of B) by DEPTH k.  K_INNER: k is contiguous in memory, and a tile is OUT rows
@@ -93,85 +92,100 @@ struct Tile {
     // eight (four) neighbouring rows lies in different banks.  Otherwise rows k .. k + 3 of each of four groups eight apart are read
     // at once, 32 bytes of each: pairs of units are moved.
     static __device__ __forceinline__ int place(int row, int u) {
-        if constexpr (K_INNER) return kUnits == 8 ? u ^ (row & 7) : u ^ ((row >> 1) & 3);
+        if constexpr (K_INNER) return kUnits == 8 ? u ^ ((row >> 1) & 7) : u ^ ((row >> 1) & 3);
         if constexpr (kUnits >= 16) return u ^ (((row & 3) | ((row >> 1) & 4)) << 1);
-        return u ^ ((row & 3) << 1);
+        if constexpr (kUnits == 8) return u ^ ((row & 3) << 1);
+        static_assert(K_INNER || kUnits == 4 || kUnits >= 8, "pairs of units to move");
+        return u ^ ((row >> 2) & 2);
     }
 
-    const char* base;   // of the tile's first row, k = 0
-    int64_t plane;      // bytes
-    int64_t k_step;     // bytes from one k tile to the next
-    uint32_t stride, width;  // bytes: of a row, and where k is not inner from the tile's first value to the end of its row
-    uint32_t off[kLoads];
-    int64_t K;          // where it is inner, in whole units: rows end in zeros as far as that
-    int64_t rows;       // of the operand from the tile's first one on, where k is inner
+    const char* at;          // the next k tile's first value
+    int64_t plane, k_step;   // bytes between the parts, and from one k tile to the next
+    uint32_t stride, end;    // bytes: of a row, and of a whole k tile's range in memory
+    uint32_t off[kLoads];    // of this thread's units
+    uint32_t to;             // where a wavefront's units go in a buffer
 
-    __device__ __forceinline__ Tile(const Operand& o, int64_t first, int64_t count, int64_t K_)
-        : K(K_INNER ? (K_ + 7) / 8 * 8 : K_) {
+    __device__ __forceinline__ Tile(const Operand& o, int64_t first, int64_t count, int64_t k0) {
         stride = (uint32_t)(o.ld * 2);
         plane = o.plane * 2;
         if constexpr (K_INNER) {
-            base = static_cast<const char*>(o.p) + first * o.ld * 2;
-            rows = min((int64_t)OUT, count - first);
+            at = static_cast<const char*>(o.p) + (first * o.ld + k0) * 2;
             k_step = DEPTH * 2;
+            end = (uint32_t)(min((int64_t)OUT, count - first) - 1) * stride + DEPTH * 2;
         } else {
-            base = static_cast<const char*>(o.p) + first * 2;
+            at = static_cast<const char*>(o.p) + (k0 * o.ld + first) * 2;
             k_step = (int64_t)DEPTH * stride;
-            width = (uint32_t)(min((int64_t)OUT, (count - first + 7) / 8 * 8) * 2);
+            end = (DEPTH - 1) * stride + (uint32_t)(min((int64_t)OUT, (count - first + 7) / 8 * 8) * 2);
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int slot = i * THREADS + threadIdx.x, row = slot / kUnits;
             off[i] = (uint32_t)row * stride + (uint32_t)place(row, slot % kUnits) * 16;
         }
+        to = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
     }
 
-    // Loads k tile t into LDS at `to`.
-    __device__ __forceinline__ void load(uint32_t to, int64_t t) const {
-        const int64_t left = K - t * DEPTH;  // > 0
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        uint32_t end;
-        if constexpr (K_INNER)
-            end = (uint32_t)(rows - 1) * stride + (uint32_t)min(left, (int64_t)DEPTH) * 2;
-        else
-            end = (uint32_t)(min(left, (int64_t)DEPTH) - 1) * stride + width;
+    // Loads the next k tile into LDS at `buffer`.  left: the values of k from there on; DEPTH or more for a whole tile.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(uint32_t buffer, int left) {
+        uint32_t size = end;
+        // rows that run along k end in zeros as far as their last unit goes; what lies behind is not theirs
+        if constexpr (!WHOLE) size -= K_INNER ? (uint32_t)(DEPTH - (left + 7) / 8 * 8) * 2 : (uint32_t)(DEPTH - left) * stride;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            const uint64_t at = reinterpret_cast<uint64_t>(base + p * plane + t * k_step);
-            const i32x4 rsrc = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)end, 0x00020000};
+            const uint64_t from = reinterpret_cast<uint64_t>(at + p * plane);
+            const i32x4 rsrc = {(int)(uint32_t)from, (int)(uint32_t)(from >> 32), (int)size, 0x00020000};
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 uint32_t o = off[i];
-                if constexpr (K_INNER) {
-                    if (left < DEPTH) {  // past the last k of a row: not the next row's values, but zeros
-                        const int slot = i * THREADS + threadIdx.x, row = slot / kUnits;
-                        if (place(row, slot % kUnits) * 8 >= left) o = kBeyond;
-                    }
+                if constexpr (!WHOLE && K_INNER) {
+                    const int slot = i * THREADS + threadIdx.x, row = slot / kUnits;
+                    if (place(row, slot % kUnits) * 8 >= left) o = kBeyond;
                 }
-                buffer_to_lds(to + p * kPart + i * THREADS * 16 + wave * 1024, rsrc, o);
+                buffer_to_lds(buffer + to + p * kPart + i * THREADS * 16, rsrc, o);
             }
         }
+        at += k_step;
     }
 
-    // The matrix instruction's operand for outer index first + lane % 16 and k = 32 s + 8 (lane / 16) .. + 7.
+    // The matrix instruction's operand: MF outer indices from `first` on, one per lane, by the s-th 512 / MF k, eight per lane.
+    template <int MF>
     static __device__ __forceinline__ s16x8 fragment(const char* part, int first, int s) {
-        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+        constexpr int GROUPS = 64 / MF;  // lanes with the same outer index
+        const int lane = threadIdx.x & 63;
         if constexpr (K_INNER) {
-            const int row = first + i;
-            return *reinterpret_cast<const s16x8*>(part + row * kRow * 2 + place(row, 4 * s + q) * 16);
+            const int row = first + lane % MF;
+            return *reinterpret_cast<const s16x8*>(part + row * kRow * 2 + place(row, GROUPS * s + lane / MF) * 16);
         } else {
             typedef __attribute__((address_space(3))) s16x4* lds4;
+            const int i = lane & 15, outer = first + (lane % MF & 16);
             s16x4 half[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int row = 32 * s + 8 * q + 4 * h + (i >> 2);
-                const char* const at = part + row * kRow * 2 + place(row, first / 8 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
+                const int row = 8 * (GROUPS * s + lane / MF) + 4 * h + (i >> 2);
+                const char* const at = part + row * kRow * 2 + place(row, outer / 8 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
                 half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
             }
             return __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
 };
+
+// Workgroup b's tile of `tiles`, -1 for none: consecutive workgroups run on different XCDs, and each of the eight takes a
+// contiguous range.
+__device__ __forceinline__ int of_xcd(int b, int tiles) {
+    const int t = (b & 7) * ((tiles + 7) / 8) + (b >> 3);
+    return t < tiles ? t : -1;
+}
+
+// Where a tile lies: groups of four rows of tiles, column by column, so that neighbours read the same rows and columns.
+struct TilePlace {
+    int i, j;
+};
+__device__ __forceinline__ TilePlace place_of(int tile, int i_tiles, int j_tiles) {
+    const int group = tile / (4 * j_tiles), rest = tile % (4 * j_tiles), rows = min(4, i_tiles - 4 * group);
+    return {4 * group + rest % rows, rest / rows};
+}
 
 // A sum that the parts could not form, as one fp32 chain.
 __device__ __forceinline__ float chain(const ProductArgs& a, int64_t i, int64_t j) {
@@ -185,227 +199,310 @@ __device__ __forceinline__ float chain(const ProductArgs& a, int64_t i, int64_t 
     return sum;
 }
 
-// `n` sums of one row, or fewer at the right edge, through the epilogue.
-template <class T, int n>
-__device__ __forceinline__ void finish(const Epilogue& e, int64_t i, int j, int J, float (&z)[n]) {
-    if (j + n <= J) {
-        if (e.bias) {
-            float b[n];
-            load_values(e.bias + j, b);
-#pragma unroll
-            for (int r = 0; r < n; ++r) z[r] += b[r];
-        }
-        if (e.Z) store_values(static_cast<T*>(e.Z) + i * e.ldz + j, z);
-        float x[n] = {};
-        if (e.R) load_values(static_cast<const T*>(e.R) + i * e.ldr + j, x);
-        activate_all(z, e.activation);
-#pragma unroll
-        for (int r = 0; r < n; ++r) z[r] += x[r];
-        store_values(static_cast<T*>(e.Y) + i * e.ldy + j, z);
-        return;
-    }
-    T *const Z = static_cast<T*>(e.Z), *const Y = static_cast<T*>(e.Y);
-#pragma unroll
-    for (int r = 0; r < n; ++r) {
-        if (j + r >= J) break;
-        if (e.bias) z[r] += e.bias[j + r];
-        if (Z) Z[i * e.ldz + j + r] = (T)z[r];
-    }
-    activate_all(z, e.activation);
-#pragma unroll
-    for (int r = 0; r < n; ++r) {
-        if (j + r >= J) break;
-        if (e.R) z[r] += (float)static_cast<const T*>(e.R)[i * e.ldr + j + r];
-        Y[i * e.ldy + j + r] = (T)z[r];
+// Asks for the LDS reads of a block between the first `products` of its matrix instructions, in `groups` groups of both.
+template <int reads, int products, int groups, int g = 0>
+__device__ __forceinline__ void interleave() {
+    if constexpr (g < groups) {
+        constexpr int r = reads * (g + 1) / groups - reads * g / groups, m = products * (g + 1) / groups - products * g / groups;
+        if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+        if constexpr (m > 0) __builtin_amdgcn_sched_group_barrier(0x008, m, 0);
+        interleave<reads, products, groups, g + 1>();
     }
 }
 
 // One tile per workgroup.  T: the matrices' type; fp32 ones are PARTS = 3 planes of bf16 (split_bf16.h).  WI x WJ wavefronts.
-template <class T, int TI, int TJ, int WI, int WJ, bool A_K, bool B_K>
+template <class T, int TI, int TJ, int WI, int WJ, int MF, int DEPTH, int STAGES, bool A_K, bool B_K>
 __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int PARTS = F32 ? 3 : 1, DEPTH = F32 ? 32 : 64, THREADS = 64 * WI * WJ;
-    constexpr int FI = TI / WI / 16, FJ = TJ / WJ / 16;
+    constexpr int PARTS = F32 ? 3 : 1, THREADS = 64 * WI * WJ;
+    constexpr int FI = TI / WI / MF, FJ = TJ / WJ / MF, STEPS = DEPTH * MF / 512;
+    typedef typename std::conditional<MF == 16, f32x4, f32x16>::type Sums;
     typedef typename std::conditional<F32, bf16, T>::type E;
     typedef Tile<TI, DEPTH, A_K, PARTS, THREADS> TileA;
     typedef Tile<TJ, DEPTH, B_K, PARTS, THREADS> TileB;
     constexpr int BUF = TileA::kBytes + TileB::kBytes;
+    constexpr int kBatch = TI * TJ > 128 * 128 ? 4 : 2;
     // the sums on their way out: a wavefront's, ROUND rows at a time
     constexpr int ROUND = TI / WI < 64 ? TI / WI : 64, COLS = TJ / WJ, PITCH = COLS + 4, OUT = WI * WJ * ROUND * PITCH * 4;
-    __shared__ __align__(1024) char lds[2 * BUF > OUT ? 2 * BUF : OUT];
+    __shared__ __align__(1024) char lds[STAGES * BUF > OUT ? STAGES * BUF : OUT];
 
-    // neighbouring tiles on one XCD: groups of four rows of tiles, column by column
-    const int64_t tiles = (int64_t)a.i_tiles * a.j_tiles;
-    const int64_t tile = xcd_tile(tiles * a.splits);
+    const int whole_blocks = (a.whole + 7) / 8 * 8, shared = a.i_tiles * a.j_tiles - a.whole;
+    const bool is_whole = (int)blockIdx.x < whole_blocks;
+    int tile = is_whole ? of_xcd(blockIdx.x, a.whole) : of_xcd(blockIdx.x - whole_blocks, shared * a.splits);
     if (tile < 0) return;
-    const int split = (int)(tile / tiles), in_split = (int)(tile % tiles);
-    const int group = in_split / (4 * a.j_tiles), rest = in_split % (4 * a.j_tiles);
-    const int group_rows = min(4, a.i_tiles - 4 * group);
-    const int64_t i0 = (int64_t)(4 * group + rest % group_rows) * TI;
-    const int j0 = rest / group_rows * TJ;
+    const int splits = is_whole ? 1 : a.splits, split = is_whole ? 0 : tile / shared, in_shared = is_whole ? 0 : tile % shared;
+    if (!is_whole) tile = a.whole + in_shared;
+    const TilePlace at = place_of(tile, a.i_tiles, a.j_tiles);
+    const int64_t i0 = (int64_t)at.i * TI;
+    const int j0 = at.j * TJ;
 
-    const TileA ta(a.A, i0, a.I, a.K);
-    const TileB tb(a.B, j0, a.J, a.K);
-    const int64_t k_tiles = (a.K + DEPTH - 1) / DEPTH;
-    const int64_t t0 = k_tiles * split / a.splits, t1 = k_tiles * (split + 1) / a.splits;
+    const int k_tiles = (int)((a.K + DEPTH - 1) / DEPTH);
+    const int t0 = (int)((int64_t)k_tiles * split / splits), stages = (int)((int64_t)k_tiles * (split + 1) / splits) - t0;
+    const int k_left = (int)min(a.K - (int64_t)t0 * DEPTH, (int64_t)stages * DEPTH), whole = k_left / DEPTH;
+    TileA ta(a.A, i0, a.I, (int64_t)t0 * DEPTH);
+    TileB tb(a.B, j0, a.J, (int64_t)t0 * DEPTH);
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
-    f32x4 sum[FI][FJ];
+    Sums sum[FI][FJ] = {};
+    struct Fragments {
+        s16x8 a[F32 ? 1 : FI], b[PARTS][FJ];
+    };
+    const auto read_a = [&](s16x8& f, int buffer, int p, int i, int s) {
+        f = TileA::template fragment<MF>(lds + buffer * BUF + p * TileA::kPart, wi + MF * i, s);
+    };
+    const auto read_b = [&](Fragments& f, int buffer, int s) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i)
+        for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-        for (int j = 0; j < FJ; ++j) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < FJ; ++j)
+                f.b[p][j] = TileB::template fragment<MF>(lds + buffer * BUF + TileA::kBytes + p * TileB::kPart, wj + MF * j, s);
+    };
 
+    // A ring of STAGES buffers, one k tile each.  While a step's products run from registers, the next step's operands are read:
+    // a stage's barrier says that the next one has arrived and that everybody has read all of this one, whose buffer is loaded anew.
     const uint32_t base = lds_offset(lds);
-    if (t0 < t1) {
-        ta.load(base, t0);
-        tb.load(base + TileA::kBytes, t0);
-    }
-    for (int64_t t = t0; t < t1; ++t) {
-        const int cur = (int)(t - t0) & 1;
+    constexpr int LOADS = PARTS * (TileA::kLoads + TileB::kLoads);
+    const auto load = [&](int buffer, int t) {
+        if (t < whole) {
+            ta.template load<true>(base + buffer * BUF, 0);
+            tb.template load<true>(base + buffer * BUF + TileA::kBytes, 0);
+        } else {
+            ta.template load<false>(base + buffer * BUF, k_left - t * DEPTH);
+            tb.template load<false>(base + buffer * BUF + TileA::kBytes, k_left - t * DEPTH);
+        }
+    };
+#pragma unroll 1
+    for (int i = 0; i < STAGES; ++i)
+        if (i < stages) load(i, i);
+    if (STAGES <= stages)
+        wait_loads<(STAGES - 1) * LOADS>();
+    else
         wait_loads<0>();
-        lds_barrier();  // everybody's loads are there, and everybody has read the other buffer
-        if (t + 1 < t1) {
-            ta.load(base + (cur ^ 1) * BUF, t + 1);
-            tb.load(base + (cur ^ 1) * BUF + TileA::kBytes, t + 1);
+    lds_barrier();
+    Fragments now, then;
+    int buffer = 0;
+    // On to stage t + 1: its buffer, and stage t's to load into.
+    const auto arrive = [&](int t, auto steady) {
+        const int from = buffer;
+        buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+        if (decltype(steady)::value || t + STAGES <= stages)
+            wait_loads<(STAGES - 2) * LOADS>();
+        else
+            wait_loads<0>();
+        lds_barrier();
+        return from;
+    };
+    const auto refill = [&](int from, int t, auto steady) {
+        if constexpr (decltype(steady)::value) {
+            ta.template load<true>(base + from * BUF, 0);
+            tb.template load<true>(base + from * BUF + TileA::kBytes, 0);
+        } else if (t + STAGES < stages) {
+            load(from, t + STAGES);
         }
-        const char* const pa = lds + cur * BUF;
-        const char* const pb = pa + TileA::kBytes;
+    };
+    constexpr int READ_A = A_K ? 1 : 2, READ_B = B_K ? 1 : 2;  // instructions per fragment
+    constexpr int PAIR = 2 / STEPS;                            // stages of two steps
+    static_assert(STEPS <= 2, "steps of a stage");
+    const auto run = [&](auto&& step) {
+        int t = 0;
+        for (; t + PAIR - 1 + STAGES < whole; t += PAIR) {
+            step(now, then, t, 0, std::true_type());
+            step(then, now, t + PAIR - 1, STEPS - 1, std::true_type());
+        }
+        for (; t + PAIR <= stages; t += PAIR) {
+            step(now, then, t, 0, std::false_type());
+            step(then, now, t + PAIR - 1, STEPS - 1, std::false_type());
+        }
+        if (t < stages) step(now, then, t, 0, std::false_type());
+    };
+    read_b(now, 0, 0);
+    if constexpr (!F32) {
+        const auto read_all_a = [&](Fragments& f, int s) {
 #pragma unroll
-        for (int s = 0; s < DEPTH / 32; ++s) {
-            if constexpr (!F32) {
-                s16x8 fa[FI], fb[FJ];
-#pragma unroll
-                for (int j = 0; j < FJ; ++j) fb[j] = TileB::fragment(pb, wj + 16 * j, s);
-#pragma unroll
-                for (int i = 0; i < FI; ++i) fa[i] = TileA::fragment(pa, wi + 16 * i, s);
-#pragma unroll
-                for (int i = 0; i < FI; ++i)
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j) sum[i][j] = mfma(fb[j], fa[i], sum[i][j], E());
-            } else {
-                constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};  // small products first
-                s16x8 fb[FJ][3];
-#pragma unroll
-                for (int j = 0; j < FJ; ++j)
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) fb[j][p] = TileB::fragment(pb + p * TileB::kPart, wj + 16 * j, s);
-#pragma unroll
-                for (int i = 0; i < FI; ++i) {
-                    s16x8 fa[3];
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) fa[p] = TileA::fragment(pa + p * TileA::kPart, wi + 16 * i, s);
-                    f32x4 slice[FJ];
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j) slice[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int n = 0; n < 6; ++n)
-#pragma unroll
-                        for (int j = 0; j < FJ; ++j) slice[j] = mfma(fb[j][kPairs[n][1]], fa[kPairs[n][0]], slice[j], E());
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j) sum[i][j] += slice[j];
-                }
+            for (int i = 0; i < FI; ++i) read_a(f.a[i], buffer, 0, i, s);
+        };
+        read_all_a(now, 0);
+        run([&](const Fragments& f, Fragments& next, int t, int s, auto steady) {
+            const bool last = s + 1 == STEPS;
+            int from = 0;
+            if (last) {
+                from = arrive(t, steady);
+                if constexpr (!decltype(steady)::value) refill(from, t, steady);
             }
-        }
+            read_b(next, buffer, last ? 0 : s + 1);  // behind the last stage: something, unused
+            read_all_a(next, last ? 0 : s + 1);
+            if constexpr (decltype(steady)::value)
+                if (last) refill(from, t, steady);
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) sum[i][j] = mfma(f.b[0][j], f.a[i], sum[i][j], E());
+            interleave<FI * READ_A + FJ * READ_B, FI * FJ, FI * FJ / 2>();
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    } else {
+        // A's fragments are read one row of them ahead, B's one stage: the last row's products hide those.
+        static_assert(STEPS == 1 && FI % 2 == 0, "two rows in turn");
+        s16x8 row[2][3];
+        const auto read_row = [&](int i) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) read_a(row[i & 1][p], buffer, p, i % FI, 0);
+        };
+        read_row(0);
+        run([&](const Fragments& f, Fragments& next, int t, int, auto steady) {
+#pragma unroll
+            for (int i = 0; i < FI; ++i) {
+                if (i + 1 == FI) {
+                    const int from = arrive(t, steady);
+                    if constexpr (!decltype(steady)::value) refill(from, t, steady);
+                    read_b(next, buffer, 0);
+                    read_row(FI);
+                    if constexpr (decltype(steady)::value) refill(from, t, steady);
+                } else {
+                    read_row(i + 1);
+                }
+                constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};  // small products first
+                Sums slice[FJ] = {};
+#pragma unroll
+                for (int n = 0; n < 6; ++n)
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) slice[j] = mfma(f.b[kPairs[n][1]][j], row[i & 1][kPairs[n][0]], slice[j], E());
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) sum[i][j] += slice[j];
+                if (i + 1 == FI)
+                    interleave<3 * (READ_A + FJ * READ_B), 6 * FJ, 3 * FJ>();
+                else
+                    interleave<3 * READ_A, 3 * FJ, 3>();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
     }
+    wait_loads<0>();
 
     // Out through LDS, so that a row's values leave in whole lines: every wavefront its own, nothing to wait for but that all
     // have read their operands.
-    lds_barrier();
-    constexpr int VEC = F32 ? 4 : 8, LANES = COLS / VEC;  // values per lane, lanes per row
+    constexpr int VEC = F32 ? 4 : 8, LANES = COLS / VEC, STEP = 64 / LANES;  // values per lane, lanes per row, rows at once
+    constexpr int BATCH = ROUND / STEP < kBatch ? ROUND / STEP : kBatch;
     const int lane = threadIdx.x & 63;
+    const int in_cols = wj + lane % LANES * VEC, col = j0 + in_cols;
+    float bias[VEC];
+    load_bias(a.e, col, a.J, bias);
+    lds_barrier();
     float* const out = reinterpret_cast<float*>(lds) + wave * ROUND * PITCH;
 #pragma unroll
     for (int round = 0; round < TI / WI / ROUND; ++round) {
+        float probe = 0.f;
 #pragma unroll
-        for (int i = 0; i < ROUND / 16; ++i)
+        for (int i = 0; i < ROUND / MF; ++i)
 #pragma unroll
-            for (int j = 0; j < FJ; ++j) {
-                f32x4 z = sum[round * ROUND / 16 + i][j];
-                if constexpr (F32) z *= kUnscale;
-                *reinterpret_cast<f32x4*>(out + (16 * i + (lane & 15)) * PITCH + 16 * j + 4 * (lane >> 4)) = z;
-            }
-        const int col = j0 + wj + lane % LANES * VEC;
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int r = 0; r < MF * MF / 64; r += 4) {  // four columns of the row that the lane has
+                    const Sums& all = sum[round * ROUND / MF + i][j];
+                    f32x4 z = {all[r], all[r + 1], all[r + 2], all[r + 3]};
+                    if constexpr (F32) {
+                        z *= kUnscale;
+                        probe += fabsf(z[0]) + fabsf(z[1]) + (fabsf(z[2]) + fabsf(z[3]));
+                    }
+                    *reinterpret_cast<f32x4*>(out + (MF * i + lane % MF) * PITCH + MF * j + 256 / MF * (r / 4) + 4 * (lane / MF)) = z;
+                }
+        if constexpr (F32)
+            // sums that are not finite are formed again: an infinite value has no parts
+            if (splits == 1 && __any(!is_finite(probe))) {
 #pragma unroll 1
-        for (int r = lane / LANES; r < ROUND; r += 64 / LANES) {
-            const int64_t row = i0 + wi + round * ROUND + r;
-            if (row >= a.I || col >= a.J) continue;
-            float z[VEC];
-            load_values(out + r * PITCH + lane % LANES * VEC, z);
-            if (a.splits > 1) {
-                float* const to = a.partial + ((int64_t)split * a.I + row) * a.J + col;
-                if (col + VEC <= a.J)
-                    store_values(to, z);
-                else
-                    for (int c = 0; c < VEC && col + c < a.J; ++c) to[c] = z[c];
+                for (int v = lane; v < ROUND * COLS; v += 64) {
+                    const int64_t i = i0 + wi + round * ROUND + v / COLS;
+                    const int j = j0 + wj + v % COLS;
+                    float& z = out[v / COLS * PITCH + v % COLS];
+                    if (i < a.I && j < a.J && !is_finite(z)) z = chain(a, i, j);
+                }
+            }
+#pragma unroll 1
+        for (int b = 0; b < ROUND / STEP; b += BATCH) {
+            float z[BATCH][VEC];
+            int64_t row[BATCH];
+            const int first = b * STEP + lane / LANES, in_rows = wi + round * ROUND + first;
+#pragma unroll
+            for (int r = 0; r < BATCH; ++r) {
+                load_values(out + (first + r * STEP) * PITCH + lane % LANES * VEC, z[r]);
+                row[r] = i0 + in_rows + r * STEP;
+            }
+            if (splits > 1) {
+                float* const to = a.partial + (((int64_t)split * shared + in_shared) * TI + in_rows) * TJ + in_cols;
+#pragma unroll
+                for (int r = 0; r < BATCH; ++r) store_values(to + r * STEP * TJ, z[r]);
                 continue;
             }
-            if constexpr (F32)
-#pragma unroll
-                for (int c = 0; c < VEC; ++c)
-                    if (!is_finite(z[c])) z[c] = chain(a, row, min(col + c, a.J - 1));
-            finish<T>(a.e, row, col, a.J, z);
+            if (row[0] >= a.I || col >= a.J) continue;
+            finish<T>(a.e, row, col, a.I, a.J, bias, z);
         }
     }
 }
 
-// The splits' sums through the epilogue, four columns per thread.
-template <class T>
+// The shared tiles' sums through the epilogue, four columns per thread.  TI x TJ: a tile.
+template <class T, int TI, int TJ>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs a) {
-    const int quads = (a.J + 3) / 4;
-    for (int64_t v = blockIdx.x * 256LL + threadIdx.x; v < a.I * quads; v += gridDim.x * 256LL) {
-        const int64_t i = v / quads;
-        const int j = (int)(v - i * quads) * 4;
+    constexpr int QUADS = TI * TJ / 4;
+    const int shared = a.i_tiles * a.j_tiles - a.whole;
+    for (int64_t v = blockIdx.x * 256LL + threadIdx.x; v < (int64_t)shared * QUADS; v += gridDim.x * 256LL) {
+        const int tile = (int)(v / QUADS), in_tile = (int)(v % QUADS) * 4;
+        const TilePlace at = place_of(a.whole + tile, a.i_tiles, a.j_tiles);
+        const int64_t i = (int64_t)at.i * TI + in_tile / TJ;
+        const int j = at.j * TJ + in_tile % TJ;
+        if (i >= a.I || j >= a.J) continue;
+        const float* from = a.partial + (int64_t)tile * TI * TJ + in_tile;
         float z[4] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            const float* const from = a.partial + ((int64_t)s * a.I + i) * a.J + j;
-            if (j + 3 < a.J) {
-                float x[4];
-                load_values(from, x);
+        for (int s = 0; s < a.splits; ++s, from += (int64_t)shared * TI * TJ) {
+            float x[4];
+            load_values(from, x);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) z[r] += x[r];
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) z[r] += j + r < a.J ? from[r] : 0.f;
-            }
+            for (int r = 0; r < 4; ++r) z[r] += x[r];
         }
         if constexpr (sizeof(T) == 4)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (!is_finite(z[r])) z[r] = chain(a, i, min(j + r, a.J - 1));
-        finish<T>(a.e, i, j, a.J, z);
+            for (int r = 0; r < 4 && j + r < a.J; ++r)
+                if (!is_finite(z[r])) z[r] = chain(a, i, j + r);
+        float bias[4], rows[1][4] = {{z[0], z[1], z[2], z[3]}};
+        load_bias(a.e, j, a.J, bias);
+        const int64_t row[1] = {i};
+        finish<T>(a.e, row, j, a.I, a.J, bias, rows);
     }
 }
 
-template <class T, int TI, int TJ, int WI, int WJ, bool A_K, bool B_K>
+// a: whole = how many tiles not to share; i_tiles and j_tiles are set here.
+template <class T, int TI, int TJ, int WI, int WJ, int MF, int DEPTH, int STAGES, bool A_K, bool B_K>
 hipError_t launch(ProductArgs a, hipStream_t s) {
-    const int64_t i_tiles = (a.I + TI - 1) / TI;
-    a.j_tiles = (a.J + TJ - 1) / TJ;
-    const int64_t blocks = (i_tiles * a.j_tiles * a.splits + 7) / 8 * 8;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    a.i_tiles = (int)i_tiles;
-    hipLaunchKernelGGL((product_kernel<T, TI, TJ, WI, WJ, A_K, B_K>), dim3((unsigned)blocks), dim3(64 * WI * WJ), 0, s, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-    const int64_t quads = (a.J + 3) / 4 * a.I;
-    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 1 << 16)), dim3(256), 0, s, a);
+    const int64_t i_tiles = (a.I + TI - 1) / TI, j_tiles = (a.J + TJ - 1) / TJ, tiles = i_tiles * j_tiles;
+    if (tiles > (1 << 30) || (tiles - a.whole) * a.splits > (1 << 30)) return hipErrorInvalidValue;
+    a.i_tiles = (int)i_tiles, a.j_tiles = (int)j_tiles;
+    const int shared = (int)tiles - a.whole;
+    const unsigned blocks = (a.whole + 7) / 8 * 8 + (shared * a.splits + 7) / 8 * 8;
+    hipLaunchKernelGGL((product_kernel<T, TI, TJ, WI, WJ, MF, DEPTH, STAGES, A_K, B_K>), dim3(blocks), dim3(64 * WI * WJ), 0, s, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || shared == 0 || a.splits == 1) return e;
+    const int64_t quads = (int64_t)shared * TI * TJ / 4;
+    hipLaunchKernelGGL((join_kernel<T, TI, TJ>), dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 1 << 16)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
+// The tiles of dense_linear.hip's list by number.
 template <class T>
 hipError_t launch_tile(int tile, bool a_k, bool b_k, const ProductArgs& a, hipStream_t s) {
     const auto with = [&](auto ak, auto bk) {
         constexpr bool AK = decltype(ak)::value, BK = decltype(bk)::value;
         if constexpr (sizeof(T) == 4) {
             switch (tile) {
-                case 0: return launch<T, 128, 128, 2, 2, AK, BK>(a, s);
-                default: return launch<T, 64, 64, 2, 2, AK, BK>(a, s);
+                case 0: return launch<T, 128, 256, 2, 4, 16, 32, 2, AK, BK>(a, s);
+                case 1: return launch<T, 128, 128, 2, 4, 16, 32, 2, AK, BK>(a, s);
+                case 2: return launch<T, 64, 128, 2, 2, 16, 32, 2, AK, BK>(a, s);
+                default: return launch<T, 64, 64, 2, 2, 16, 32, 2, AK, BK>(a, s);
             }
         } else {
             switch (tile) {
-                case 0: return launch<T, 256, 256, 2, 4, AK, BK>(a, s);
-                case 1: return launch<T, 128, 128, 2, 2, AK, BK>(a, s);
-                default: return launch<T, 64, 64, 2, 2, AK, BK>(a, s);
+                case 0: return launch<T, 256, 256, 2, 4, 16, 32, 3, AK, BK>(a, s);
+                case 1: return launch<T, 128, 128, 2, 4, 16, 64, 2, AK, BK>(a, s);
+                case 2: return launch<T, 64, 128, 2, 4, 16, 64, 2, AK, BK>(a, s);
+                case 3: return launch<T, 64, 64, 2, 2, 16, 64, 3, AK, BK>(a, s);
+                default: return launch<T, 32, 64, 1, 4, 16, 64, 3, AK, BK>(a, s);
             }
         }
     };
