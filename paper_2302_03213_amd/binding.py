@@ -762,6 +762,10 @@ def dense_linear(X, W, bias=None, activation=None, residual=None, out=None, prea
     """lutnn_dense_linear: Y = activation(X @ W + bias) + residual.  X [N, D], W [D, M] and residual [N, M] of one type (fp32,
     bf16, fp16), bias [M] fp32; activation None, "relu", "gelu", "gelu_tanh" or "silu".  preactivation: an [N, M] tensor that
     receives X @ W + bias, as dense_linear_backward wants it."""
+    if out is None:
+        got = _calls.dense_linear(X, W, bias, ACTIVATIONS.get(activation, -1), residual, preactivation)
+        if got is not None:
+            return _result(got)
     dtype, act = _typed("X", X), _activation(activation)
     (N, D), M = X.shape, W.shape[-1]
     ldx, ldw = _matrix("X", X, (N, D), X), _matrix("W", W, (D, M), X)
@@ -783,6 +787,9 @@ def dense_linear(X, W, bias=None, activation=None, residual=None, out=None, prea
 def dense_linear_backward(X, W, G, preactivation=None, activation=None, need_dx=True, need_dw=True, need_dbias=True):
     """lutnn_dense_linear_backward: the gradients of dense_linear from G = dL/dY [N, M].  Returns (dX [N, D], dW [D, M], dbias [M]
     fp32), None for what is not needed.  The residual's gradient is G itself."""
+    got = _calls.dense_linear_backward(X, W, G, preactivation, ACTIVATIONS.get(activation, -1), need_dx, need_dw, need_dbias)
+    if got is not None:
+        return _result(got)
     dtype, act = _typed("G", G), _activation(activation)
     (N, M), D = G.shape, W.shape[0]
     ldx, ldw, ldg = _matrix("X", X, (N, D), G), _matrix("W", W, (D, M), G), _matrix("G", G, (N, M), G)
@@ -806,6 +813,10 @@ def layer_norm(X, weight=None, bias=None, eps=1e-5, residual=None, out=None, tot
     """lutnn_layer_norm: the rows of S = X + residual, normalised, times weight, plus bias.  X [N, D] and residual of one type
     (fp32, bf16, fp16), weight and bias [D] fp32.  total: an [N, D] tensor that receives S; statistics: an [N, 2] fp32 tensor that
     receives the rows' mean and 1 / sqrt(variance + eps), as layer_norm_backward wants them."""
+    if out is None:
+        got = _calls.layer_norm(X, weight, bias, eps, residual, total, statistics)
+        if got is not None:
+            return _result(got)
     dtype = _typed("X", X)
     N, D = X.shape
     ldx = _matrix("X", X, (N, D), X)
@@ -834,6 +845,9 @@ def layer_norm_backward(G, X, statistics, weight=None, residual=None, need_dx=Tr
     """lutnn_layer_norm_backward: the gradients of layer_norm from G = dL/dY [N, D]; X is what was normalised (the total, where
     there was a residual).  residual: a gradient [N, D] that reaches X by another way and is added to dX.  Returns (dX [N, D],
     dweight [D], dbias [D]), the vectors fp32, None for what is not needed."""
+    got = _calls.layer_norm_backward(G, X, statistics, weight, residual, need_dx, need_dweight, need_dbias)
+    if got is not None:
+        return _result(got)
     dtype = _typed("G", G)
     N, D = G.shape
     ldg, ldx = _matrix("G", G, (N, D), G), _matrix("X", X, (N, D), G)

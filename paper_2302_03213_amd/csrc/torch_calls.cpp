@@ -2,7 +2,7 @@
 // and scratch allocated, pointers taken and the launch made in one native call (a linear layer's host time 7.6 -> 5 us, of
 // which two launches in flight are 4).
 //
-// Each function takes the plain case only - CUDA fp32 tensors of the layout that the call wants - and returns None for
+// Each function takes the plain case only - CUDA tensors of the type and layout that the call wants - and returns None for
 // anything else, which binding.py then takes the long way, with that way's checks and errors.  A status other than 0 comes
 // back as an int.
 #include <torch/csrc/autograd/python_variable.h>
@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <utility>
 
 #include "lutnn.h"
 
@@ -22,18 +23,19 @@ const lutnn_tree* tree_of(PyObject* address) { return static_cast<const lutnn_tr
 
 void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
-// An ordinary CUDA tensor of fp32 with `dims` dimensions: no subclass, no transform's wrapper, no forward-mode tangent (which
+// An ordinary CUDA tensor of `type` with `dims` dimensions: no subclass, no transform's wrapper, no forward-mode tangent (which
 // what the long way leaves to torch carries on).
-bool plain(PyObject* object, int64_t dims) {
+bool plain(PyObject* object, int64_t dims, at::ScalarType type = at::kFloat) {
     if (!THPVariable_CheckExact(object) && Py_TYPE(object) != reinterpret_cast<PyTypeObject*>(ParameterClass)) return false;
     const at::Tensor& t = THPVariable_Unpack(object);
     static constexpr c10::DispatchKeySet kWrapped({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched,
                                                    c10::DispatchKey::FuncTorchGradWrapper, c10::DispatchKey::Batched,
                                                    c10::DispatchKey::Functionalize, c10::DispatchKey::ZeroTensor,
                                                    c10::DispatchKey::Negative});
-    return t.is_cuda() && t.scalar_type() == at::kFloat && t.dim() == dims && t.layout() == at::kStrided &&
+    return t.is_cuda() && t.scalar_type() == type && t.dim() == dims && t.layout() == at::kStrided &&
            !t.key_set().has_any(kWrapped) && !t._fw_grad(0).defined();
 }
+bool here(const at::Tensor& t) { return t.get_device() == c10::hip::current_device(); }
 bool rows(PyObject* object) { return plain(object, 2) && THPVariable_Unpack(object).stride(1) == 1; }
 bool dense(PyObject* object, int64_t dims) { return plain(object, dims) && THPVariable_Unpack(object).is_contiguous(); }
 
@@ -256,11 +258,161 @@ PyObject* bias_gradient(PyObject* const* args, Py_ssize_t n) {
     return result(launch([=] { return lutnn_bias_gradient(g, outer, ldg, (int32_t)M, inner, y, w, size, s); }), out);
 }
 
+// ---- the layers between the looked-up ones
+
+// A matrix of `type` on the current device, [rows][cols], its rows contiguous; or None, where that is allowed.
+bool given(PyObject* object) { return object != Py_None; }
+bool matrix(PyObject* object, at::ScalarType type, int64_t rows, int64_t cols) {
+    if (!plain(object, 2, type)) return false;
+    const at::Tensor& t = THPVariable_Unpack(object);
+    return t.size(0) == rows && t.size(1) == cols && (t.size(1) <= 1 || t.size(0) == 0 || t.stride(1) == 1) && here(t);
+}
+bool vector(PyObject* object, int64_t length) {
+    if (!plain(object, 1, at::kFloat)) return false;
+    const at::Tensor& t = THPVariable_Unpack(object);
+    return t.size(0) == length && t.is_contiguous() && here(t);
+}
+bool statistics_of(PyObject* object, int64_t rows) {
+    return matrix(object, at::kFloat, rows, 2) && THPVariable_Unpack(object).is_contiguous();
+}
+
+// Its type as a lutnn_dtype, -1 for none.
+int dtype_of(PyObject* object) {
+    for (const auto [type, code] : {std::pair(at::kFloat, LUTNN_F32), std::pair(at::kBFloat16, LUTNN_BF16), std::pair(at::kHalf, LUTNN_F16)})
+        if (plain(object, 2, type)) return code;
+    return -1;
+}
+
+struct Rows {
+    void* p = nullptr;
+    int64_t ld = 0;
+};
+// A single row has no stride.
+Rows rows_of(const at::Tensor& t) { return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : t.size(1)}; }
+Rows rows_of(PyObject* object) { return given(object) ? rows_of(THPVariable_Unpack(object)) : Rows(); }
+float* vector_of(PyObject* object) { return given(object) ? data(object) : nullptr; }
+
+PyObject* wrap(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : none(); }
+
+// dense_linear(X, W, bias, activation, residual, preactivation): Y
+PyObject* dense_linear(PyObject* const* args, Py_ssize_t n) {
+    if (n != 6 || !PyLong_CheckExact(args[3])) return none();
+    const int dtype = dtype_of(args[0]);
+    if (dtype < 0) return none();
+    const at::Tensor& X = THPVariable_Unpack(args[0]);
+    const at::ScalarType type = X.scalar_type();
+    if (!plain(args[1], 2, type)) return none();
+    const at::Tensor& W = THPVariable_Unpack(args[1]);
+    const int64_t N = X.size(0), D = X.size(1), M = W.size(1);
+    const long activation = PyLong_AsLong(args[3]);
+    if (D > INT32_MAX || M > INT32_MAX || activation < 0 || activation > LUTNN_ACTIVATION_SILU) return none();
+    if (!matrix(args[0], type, N, D) || !matrix(args[1], type, D, M) || (given(args[2]) && !vector(args[2], M))) return none();
+    for (int i : {4, 5})
+        if (given(args[i]) && !matrix(args[i], type, N, M)) return none();
+    const Rows x = rows_of(X), w = rows_of(W), r = rows_of(args[4]), z = rows_of(args[5]);
+    const float* const bias = vector_of(args[2]);
+    const at::Tensor Y = empty({N, M}, X, type);
+    const size_t bytes = lutnn_dense_linear_workspace_bytes(dtype, x.p, N, x.ld, w.p, w.ld, (int32_t)D, (int32_t)M);
+    const at::Tensor workspace = bytes ? empty({(int64_t)bytes}, X, at::kByte) : at::Tensor();
+    void *y = Y.data_ptr(), *ws = bytes ? workspace.data_ptr() : nullptr, *s = stream();
+    return result(launch([=] {
+                      return lutnn_dense_linear(dtype, x.p, N, x.ld, w.p, w.ld, (int32_t)D, (int32_t)M, bias, (int32_t)activation, r.p, r.ld,
+                                                y, M, z.p, z.ld, ws, bytes, s);
+                  }),
+                  Y);
+}
+
+// dense_linear_backward(X, W, G, preactivation, activation, need_dx, need_dw, need_dbias): (dX, dW, dbias)
+PyObject* dense_linear_backward(PyObject* const* args, Py_ssize_t n) {
+    if (n != 8 || !PyLong_CheckExact(args[4])) return none();
+    const int dtype = dtype_of(args[2]);
+    if (dtype < 0) return none();
+    const at::Tensor& G = THPVariable_Unpack(args[2]);
+    const at::ScalarType type = G.scalar_type();
+    if (!plain(args[1], 2, type)) return none();
+    const at::Tensor& W = THPVariable_Unpack(args[1]);
+    const int64_t N = G.size(0), M = G.size(1), D = W.size(0);
+    const long activation = PyLong_AsLong(args[4]);
+    if (D > INT32_MAX || M > INT32_MAX || activation < 0 || activation > LUTNN_ACTIVATION_SILU) return none();
+    if (!matrix(args[0], type, N, D) || !matrix(args[1], type, D, M) || !matrix(args[2], type, N, M)) return none();
+    if (activation && !(given(args[3]) && matrix(args[3], type, N, M))) return none();
+    for (int i : {5, 6, 7})
+        if (!PyBool_Check(args[i])) return none();
+    const bool need_dx = args[5] == Py_True, need_dw = args[6] == Py_True, need_db = args[7] == Py_True;
+    const Rows x = rows_of(args[0]), w = rows_of(W), g = rows_of(G), z = activation ? rows_of(args[3]) : Rows();
+    const at::Tensor dX = need_dx ? empty({N, D}, G, type) : at::Tensor(), dW = need_dw ? empty({D, M}, G, type) : at::Tensor(),
+                     db = need_db ? empty({M}, G) : at::Tensor();
+    const size_t bytes = lutnn_dense_linear_backward_workspace_bytes(dtype, x.p, N, x.ld, w.p, w.ld, (int32_t)D, (int32_t)M, g.p, g.ld, z.p,
+                                                                     z.ld, (int32_t)activation, need_dx, need_dw, need_db);
+    const at::Tensor workspace = bytes ? empty({(int64_t)bytes}, G, at::kByte) : at::Tensor();
+    void *dx = need_dx ? dX.data_ptr() : nullptr, *dw = need_dw ? dW.data_ptr() : nullptr, *ws = bytes ? workspace.data_ptr() : nullptr,
+         *s = stream();
+    float* const b = data(db);
+    const int status = launch([=] {
+        return lutnn_dense_linear_backward(dtype, x.p, N, x.ld, w.p, w.ld, (int32_t)D, (int32_t)M, g.p, g.ld, z.p, z.ld, (int32_t)activation,
+                                           dx, D, dw, M, b, ws, bytes, s);
+    });
+    if (status) return PyLong_FromLong(status);
+    return Py_BuildValue("NNN", wrap(dX), wrap(dW), wrap(db));
+}
+
+// layer_norm(X, weight, bias, eps, residual, total, statistics): Y
+PyObject* layer_norm(PyObject* const* args, Py_ssize_t n) {
+    if (n != 7 || !PyFloat_CheckExact(args[3])) return none();
+    const int dtype = dtype_of(args[0]);
+    if (dtype < 0) return none();
+    const at::Tensor& X = THPVariable_Unpack(args[0]);
+    const at::ScalarType type = X.scalar_type();
+    const int64_t N = X.size(0), D = X.size(1);
+    if (D > INT32_MAX || !matrix(args[0], type, N, D) || (given(args[6]) && !statistics_of(args[6], N))) return none();
+    for (int i : {1, 2})
+        if (given(args[i]) && !vector(args[i], D)) return none();
+    for (int i : {4, 5})
+        if (given(args[i]) && !matrix(args[i], type, N, D)) return none();
+    const Rows x = rows_of(X), r = rows_of(args[4]), t = rows_of(args[5]);
+    const float *const w = vector_of(args[1]), *const b = vector_of(args[2]);
+    float* const st = vector_of(args[6]);
+    const float eps = (float)PyFloat_AsDouble(args[3]);
+    const at::Tensor Y = empty({N, D}, X, type);
+    void *y = Y.data_ptr(), *s = stream();
+    return result(launch([=] { return lutnn_layer_norm(dtype, x.p, N, x.ld, (int32_t)D, r.p, r.ld, w, b, eps, y, D, t.p, t.ld, st, s); }), Y);
+}
+
+// layer_norm_backward(G, X, statistics, weight, residual, need_dx, need_dweight, need_dbias): (dX, dweight, dbias)
+PyObject* layer_norm_backward(PyObject* const* args, Py_ssize_t n) {
+    if (n != 8) return none();
+    const int dtype = dtype_of(args[0]);
+    if (dtype < 0) return none();
+    const at::Tensor& G = THPVariable_Unpack(args[0]);
+    const at::ScalarType type = G.scalar_type();
+    const int64_t N = G.size(0), D = G.size(1);
+    if (D > INT32_MAX || !matrix(args[0], type, N, D) || !matrix(args[1], type, N, D) || !statistics_of(args[2], N)) return none();
+    if ((given(args[3]) && !vector(args[3], D)) || (given(args[4]) && !matrix(args[4], type, N, D))) return none();
+    for (int i : {5, 6, 7})
+        if (!PyBool_Check(args[i])) return none();
+    const bool need_dx = args[5] == Py_True, need_dw = args[6] == Py_True, need_db = args[7] == Py_True;
+    const Rows g = rows_of(G), x = rows_of(args[1]), r = rows_of(args[4]);
+    const float *const st = data(args[2]), *const w = vector_of(args[3]);
+    const at::Tensor dX = need_dx ? empty({N, D}, G, type) : at::Tensor(), dW = need_dw ? empty({D}, G) : at::Tensor(),
+                     db = need_db ? empty({D}, G) : at::Tensor();
+    const size_t bytes = need_dw || need_db ? lutnn_layer_norm_backward_workspace_bytes(N, (int32_t)D) : 0;
+    const at::Tensor workspace = bytes ? empty({(int64_t)bytes}, G, at::kByte) : at::Tensor();
+    void *dx = need_dx ? dX.data_ptr() : nullptr, *ws = bytes ? workspace.data_ptr() : nullptr, *s = stream();
+    float *const dw = data(dW), *const b = data(db);
+    const int status = launch([=] {
+        return lutnn_layer_norm_backward(dtype, g.p, N, g.ld, x.p, x.ld, (int32_t)D, st, w, r.p, r.ld, dx, D, dw, b, ws, bytes, s);
+    });
+    if (status) return PyLong_FromLong(status);
+    return Py_BuildValue("NNN", wrap(dX), wrap(dW), wrap(db));
+}
+
 PyMethodDef kMethods[] = {
 #define LUTNN_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
     LUTNN_METHOD(linear),          LUTNN_METHOD(linear_tree16),   LUTNN_METHOD(conv2d),
     LUTNN_METHOD(build_table),     LUTNN_METHOD(linear_gradient), LUTNN_METHOD(softpq_backward),
-    LUTNN_METHOD(softpq_backward_conv2d), LUTNN_METHOD(bias_gradient), {nullptr, nullptr, 0, nullptr}};
+    LUTNN_METHOD(softpq_backward_conv2d), LUTNN_METHOD(bias_gradient),
+    LUTNN_METHOD(dense_linear),    LUTNN_METHOD(dense_linear_backward), LUTNN_METHOD(layer_norm), LUTNN_METHOD(layer_norm_backward),
+    {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "torch_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
