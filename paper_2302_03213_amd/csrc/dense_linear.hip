@@ -7,6 +7,7 @@
 // bf16 parts, 16-bit ones of odd widths, strides or addresses as copies with padded rows.  dZ is formed on the way there, and summed
 // for db in the same pass.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "dense_product.h"
@@ -171,17 +172,17 @@ hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db
 // what a compute unit gets from L2 (75 GB/s), the large ones by the matrix instructions and the power they draw.
 struct TileSize {
     int i, j, depth, at_once;
-    float stage[4], rest[4];
+    float stage[4], rest[4], by_rows = 1.f;
 };
 constexpr TileSize kTiles16[] = {{256, 256, 32, 1, {1.55f}, {9.0f}},
                                  {128, 128, 64, 2, {0.78f, 0.90f}, {2.0f, 5.0f}},
                                  {64, 128, 64, 2, {0.61f, 0.65f}, {0.5f, 2.5f}},
                                  {64, 64, 64, 3, {0.23f, 0.46f, 0.66f}, {1.0f, 0.7f, 1.0f}},
                                  {32, 64, 64, 4, {0.16f, 0.37f, 0.56f, 0.72f}, {1.0f, 0.5f, 0.5f, 0.5f}}};
-constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {4.2f}, {12.0f}},
-                                  {128, 128, 32, 1, {2.4f}, {4.5f}},
-                                  {64, 128, 32, 2, {2.0f, 2.6f}, {0.5f, 5.5f}},
-                                  {64, 64, 32, 3, {1.4f, 1.65f, 2.4f}, {0.0f, 1.5f, 4.0f}}};
+constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {4.1f}, {12.0f}, 1.05f},
+                                  {128, 128, 32, 1, {2.35f}, {4.5f}, 1.10f},
+                                  {64, 128, 32, 2, {1.9f, 2.5f}, {0.5f, 5.5f}, 1.16f},
+                                  {64, 64, 32, 3, {1.4f, 1.5f, 2.3f}, {0.0f, 3.0f, 5.0f}, 1.2f}};
 constexpr float kLaunchUs = 2.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
 
 // A product's tile, how many of its tiles are one workgroup's, and how many workgroups share the sum of each of the others.
@@ -191,35 +192,36 @@ struct Plan {
     float us;
 };
 
-float tiles_us(const TileSize& t, int64_t count, float stages) {
-    const int64_t units = compute_units(), rounds = count / (units * t.at_once), rest = count - rounds * units * t.at_once;
+float tiles_us(const TileSize& t, float count, float stages, float units) {
+    const float rounds = std::floor(count / (units * t.at_once)), rest = count - rounds * units * t.at_once;
     float us = rounds * (stages * t.stage[t.at_once - 1] + t.rest[t.at_once - 1]);
     if (rest > 0) {
-        const int n = (int)((rest + units - 1) / units) - 1;
+        const int n = std::min((int)std::ceil(rest / units), t.at_once) - 1;
         us += stages * t.stage[n] + t.rest[n];
     }
     return us;
 }
 
 // The fastest by those figures.  A sum is shared out where the last tiles would leave most of the chip idle for longer than a second
-// launch, which adds up what the first left in memory, takes.
-Plan plan(int dtype, int64_t I, int J, int64_t K) {
+// launch, which adds up what the first left in memory, takes.  k_rows: how many of the two operands run along k; laid-out fp32 ones
+// are read in pieces of 64 bytes then, which takes small tiles a sixth longer.
+Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
-    const int count = dtype == 0 ? 4 : 5;
+    const int count = dtype == 0 ? 4 : 5, units = compute_units();
     Plan best = {0, 0, 1, 0, 1e30f};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
-        const float stage = t.depth / 64.f;
-        const float us = kLaunchUs + tiles_us(t, tiles, k_tiles * stage);
+        const float stage = t.depth / 64.f * (dtype == 0 && k_rows == 2 ? t.by_rows : 1.f);
+        const float us = kLaunchUs + tiles_us(t, (float)tiles, k_tiles * stage, (float)units);
         if (us < best.us) best = {i, (int)std::min<int64_t>(tiles, 1 << 30), 1, tiles, us};
-        const int64_t slots = compute_units() * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
-        const float base = kLaunchUs + kJoinUs + tiles_us(t, whole, k_tiles * stage);
-        if (shared == 0 || base >= best.us) continue;
+        const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
+        const float base = kLaunchUs + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
+        if (shared == 0) continue;
         for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (splits > k_tiles) break;
-            const float bytes = 2.f * splits * shared * t.i * t.j * 4;
-            const float shared_us = base + tiles_us(t, shared * splits, (float)((k_tiles + splits - 1) / splits) * stage) + bytes / kBytesPerUs;
+            const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / kBytesPerUs;
+            if (splits > k_tiles || moved >= best.us) break;
+            const float shared_us = moved + tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units);
             if (shared_us < best.us) best = {i, (int)whole, splits, tiles, shared_us};
         }
     }
@@ -286,11 +288,11 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     GradientPlan g = {};
     float tiles = 0.f, plain = 0.f, values = (float)c.N * c.M;
     if (need_dx) {
-        g.to_x = plan(c.dtype, c.N, c.D, c.M);
+        g.to_x = plan(c.dtype, c.N, c.D, c.M, 2);
         tiles += g.to_x.us, plain += plain_f32_us(c.N, c.D, c.M), values += (float)c.D * c.M;
     }
     if (need_dw) {
-        g.to_w = plan(c.dtype, c.D, c.M, c.N);
+        g.to_w = plan(c.dtype, c.D, c.M, c.N, 0);
         tiles += g.to_w.us, plain += plain_f32_us(c.D, c.M, c.N), values += (float)c.N * c.D;
     }
     g.plain = c.dtype == 0 && plain < tiles + lay_out_us(values);
@@ -323,7 +325,7 @@ ForwardPlan forward_plan(const DenseCall& c) {
     ForwardPlan f = {};
     f.few = c.N <= kFewRows;
     if (f.few) return f;
-    f.product = plan(c.dtype, c.N, c.M, c.D);
+    f.product = plan(c.dtype, c.N, c.M, c.D, 1);
     f.plain = c.dtype == 0 && plain_f32_us(c.N, c.M, c.D) < f.product.us + lay_out_us((float)c.N * c.D + (float)c.D * c.M);
     f.x = !f.plain && !usable(c.dtype, c.X, c.ldx, c.D);
     f.w = !f.plain && !usable(c.dtype, c.W, c.ldw, c.M);

@@ -103,7 +103,7 @@ __device__ __forceinline__ f32x4 four(const PlainOperand& o, int64_t outer, int6
 template <int FI, bool A_K, bool B_K>
 __global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainOperand A, PlainOperand B, int64_t I, int J, int64_t K, int row_blocks,
                                                              int strips, Epilogue e) {
-    constexpr int AHEAD = 2;
+    constexpr int AHEAD = FI == 1 ? 4 : 2;
     __shared__ float part[kWaves][FI * 16][kCols + 1];
     const int block = strip_of(blockIdx.x, row_blocks * strips);
     if (block < 0) return;
@@ -131,8 +131,8 @@ __global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainOperand A, Pla
                 for (int i = 0; i < FI; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[u][r], a[u][i][r], sum[i], 0, 0, 0);
     };
     int64_t k = 16 * wave;
-    for (; k + 16 * kWaves < K; k += AHEAD * 16 * kWaves) add(std::integral_constant<int, AHEAD>(), k);
-    if (k < K) add(std::integral_constant<int, 1>(), k);
+    for (; k + (AHEAD / 2) * 16 * kWaves < K; k += AHEAD * 16 * kWaves) add(std::integral_constant<int, AHEAD>(), k);
+    if (k < K) add(std::integral_constant<int, AHEAD / 2>(), k);
     // the first operand's index is the instruction's row: a lane has columns 4 q .. 4 q + 3 of row i16
 #pragma unroll
     for (int i = 0; i < FI; ++i)
@@ -151,7 +151,11 @@ __global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainOperand A, Pla
     }
 }
 
-int row_fragments(int64_t I) { return (int)std::min<int64_t>((I + 15) / 16, 4); }
+// Row fragments per workgroup: up to four, which read a strip of W once for all of them, but a workgroup for every compute unit first.
+int row_fragments(int64_t I, int J, int units) {
+    const int64_t strips = (J + kCols - 1) / kCols, fragments = (I + 15) / 16;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(4, fragments * strips / units));
+}
 
 }  // namespace
 
@@ -171,7 +175,7 @@ hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, con
 }
 
 hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_t I, int J, int64_t K, const Epilogue& e, hipStream_t s) {
-    const int fragments = row_fragments(I), strips = (J + kCols - 1) / kCols;
+    const int fragments = row_fragments(I, J, compute_units()), strips = (J + kCols - 1) / kCols;
     const int64_t row_blocks = (I + 16 * fragments - 1) / (16 * fragments);
     if (row_blocks * strips > (1 << 30)) return hipErrorInvalidValue;
     const auto with = [&](auto fi) {
@@ -192,11 +196,11 @@ hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_
     }
 }
 
-// A launch, and per compute unit and 64 x 16 block 4.4 ns per k.
+// A launch, and 2.3 ns per k, fragment and round of workgroups.
 float plain_f32_us(int64_t I, int J, int64_t K) {
-    const int fragments = row_fragments(I);
+    const int units = compute_units(), fragments = row_fragments(I, J, units);
     const int64_t blocks = ((I + 16 * fragments - 1) / (16 * fragments)) * ((J + kCols - 1) / kCols);
-    return 3.5f + (float)((blocks + compute_units() - 1) / compute_units()) * K * 0.0011f * (fragments + 0.25f);
+    return 4.f + (float)((blocks + units - 1) / units) * K * 0.0023f * (fragments + 0.25f);
 }
 
 }  // namespace lutnn
