@@ -182,7 +182,7 @@ constexpr TileSize kTiles16[] = {{256, 256, 32, 1, {1.55f}, {9.0f}},
 constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {4.1f}, {12.0f}, 1.05f},
                                   {128, 128, 32, 1, {2.35f}, {4.5f}, 1.10f},
                                   {64, 128, 32, 2, {1.9f, 2.5f}, {0.5f, 5.5f}, 1.16f},
-                                  {64, 64, 32, 3, {1.4f, 1.5f, 2.3f}, {0.0f, 3.0f, 5.0f}, 1.2f}};
+                                  {64, 64, 32, 3, {1.4f, 1.7f, 2.7f}, {0.0f, 3.0f, 5.0f}, 1.2f}};
 constexpr float kLaunchUs = 2.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
 
 // A product's tile, how many of its tiles are one workgroup's, and how many workgroups share the sum of each of the others.

@@ -36,7 +36,6 @@ struct ProductArgs {
 namespace product {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -49,13 +48,6 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, bf16) {
 }
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
-__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c, bf16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c, f16) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 // Orders the workgroup's LDS operations only: loads to LDS stay in flight.
@@ -87,6 +79,7 @@ struct Tile {
     static constexpr int kBytes = kPart * PARTS;
     static constexpr int kLoads = kPart / (THREADS * 16);          // per thread and part
     static_assert(kPart % (THREADS * 16) == 0, "whole loads");
+    static_assert(K_INNER ? kUnits == 4 || kUnits == 8 : kUnits >= 4, "units to move");
 
     // Where unit u of a row lies in it.  k inner: rows of 128 or 64 bytes, read 16 of them at a time at one unit; the same unit of
     // eight (four) neighbouring rows lies in different banks.  Otherwise rows k .. k + 3 of each of four groups eight apart are read
@@ -95,7 +88,6 @@ struct Tile {
         if constexpr (K_INNER) return kUnits == 8 ? u ^ ((row >> 1) & 7) : u ^ ((row >> 1) & 3);
         if constexpr (kUnits >= 16) return u ^ (((row & 3) | ((row >> 1) & 4)) << 1);
         if constexpr (kUnits == 8) return u ^ ((row & 3) << 1);
-        static_assert(K_INNER || kUnits == 4 || kUnits >= 8, "pairs of units to move");
         return u ^ ((row >> 2) & 2);
     }
 
@@ -148,22 +140,19 @@ struct Tile {
         at += k_step;
     }
 
-    // The matrix instruction's operand: MF outer indices from `first` on, one per lane, by the s-th 512 / MF k, eight per lane.
-    template <int MF>
+    // The matrix instruction's operand: 16 outer indices from `first` on, one per lane, by the s-th 32 k, eight per lane.
     static __device__ __forceinline__ s16x8 fragment(const char* part, int first, int s) {
-        constexpr int GROUPS = 64 / MF;  // lanes with the same outer index
-        const int lane = threadIdx.x & 63;
+        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
         if constexpr (K_INNER) {
-            const int row = first + lane % MF;
-            return *reinterpret_cast<const s16x8*>(part + row * kRow * 2 + place(row, GROUPS * s + lane / MF) * 16);
+            const int row = first + i;
+            return *reinterpret_cast<const s16x8*>(part + row * kRow * 2 + place(row, 4 * s + q) * 16);
         } else {
             typedef __attribute__((address_space(3))) s16x4* lds4;
-            const int i = lane & 15, outer = first + (lane % MF & 16);
             s16x4 half[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = 8 * (GROUPS * s + lane / MF) + 4 * h + (i >> 2);
-                const char* const at = part + row * kRow * 2 + place(row, outer / 8 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
+            for (int h = 0; h < 2; ++h) {  // lane i gets column i of the four rows of 16 values that its 16 lanes name
+                const int row = 32 * s + 8 * q + 4 * h + (i >> 2);
+                const char* const at = part + row * kRow * 2 + place(row, first / 8 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
                 half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
             }
             return __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -211,12 +200,11 @@ __device__ __forceinline__ void interleave() {
 }
 
 // One tile per workgroup.  T: the matrices' type; fp32 ones are PARTS = 3 planes of bf16 (split_bf16.h).  WI x WJ wavefronts.
-template <class T, int TI, int TJ, int WI, int WJ, int MF, int DEPTH, int STAGES, bool A_K, bool B_K>
+template <class T, int TI, int TJ, int WI, int WJ, int DEPTH, int STAGES, bool A_K, bool B_K>
 __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int PARTS = F32 ? 3 : 1, THREADS = 64 * WI * WJ;
-    constexpr int FI = TI / WI / MF, FJ = TJ / WJ / MF, STEPS = DEPTH * MF / 512;
-    typedef typename std::conditional<MF == 16, f32x4, f32x16>::type Sums;
+    constexpr int FI = TI / WI / 16, FJ = TJ / WJ / 16, STEPS = DEPTH / 32;
     typedef typename std::conditional<F32, bf16, T>::type E;
     typedef Tile<TI, DEPTH, A_K, PARTS, THREADS> TileA;
     typedef Tile<TJ, DEPTH, B_K, PARTS, THREADS> TileB;
@@ -244,19 +232,19 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave / WJ * (TI / WI), wj = wave % WJ * (TJ / WJ);
-    Sums sum[FI][FJ] = {};
+    f32x4 sum[FI][FJ] = {};
     struct Fragments {
         s16x8 a[F32 ? 1 : FI], b[PARTS][FJ];
     };
     const auto read_a = [&](s16x8& f, int buffer, int p, int i, int s) {
-        f = TileA::template fragment<MF>(lds + buffer * BUF + p * TileA::kPart, wi + MF * i, s);
+        f = TileA::fragment(lds + buffer * BUF + p * TileA::kPart, wi + 16 * i, s);
     };
     const auto read_b = [&](Fragments& f, int buffer, int s) {
 #pragma unroll
         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
             for (int j = 0; j < FJ; ++j)
-                f.b[p][j] = TileB::template fragment<MF>(lds + buffer * BUF + TileA::kBytes + p * TileB::kPart, wj + MF * j, s);
+                f.b[p][j] = TileB::fragment(lds + buffer * BUF + TileA::kBytes + p * TileB::kPart, wj + 16 * j, s);
     };
 
     // A ring of STAGES buffers, one k tile each.  While a step's products run from registers, the next step's operands are read:
@@ -363,7 +351,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
                     read_row(i + 1);
                 }
                 constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};  // small products first
-                Sums slice[FJ] = {};
+                f32x4 slice[FJ] = {};
 #pragma unroll
                 for (int n = 0; n < 6; ++n)
 #pragma unroll
@@ -388,25 +376,34 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
     const int in_cols = wj + lane % LANES * VEC, col = j0 + in_cols;
     float bias[VEC];
     load_bias(a.e, col, a.J, bias);
+    // A residual without an activation, in whole units: all of it is asked for at once, into registers that held operands.  Batch by
+    // batch each would wait for its own.
+    constexpr int PER = ROUND / STEP, ROUNDS = TI / WI / ROUND;
+    const bool added = splits == 1 && a.e.R && a.e.activation == kActNone && !a.e.Z;
+    typename Packed<T, VEC>::type residual[ROUNDS * PER];
+    if (added)
+#pragma unroll
+        for (int r = 0; r < ROUNDS * PER; ++r) {
+            const int64_t row = min(i0 + wi + r * STEP + lane / LANES, a.I - 1);
+            const T* const from = static_cast<const T*>(a.e.R) + row * a.e.ldr + col;
+            if (col + VEC <= a.J) residual[r] = *reinterpret_cast<const typename Packed<T, VEC>::type*>(from);
+        }
     lds_barrier();
     float* const out = reinterpret_cast<float*>(lds) + wave * ROUND * PITCH;
 #pragma unroll
-    for (int round = 0; round < TI / WI / ROUND; ++round) {
+    for (int round = 0; round < ROUNDS; ++round) {
         float probe = 0.f;
 #pragma unroll
-        for (int i = 0; i < ROUND / MF; ++i)
+        for (int i = 0; i < ROUND / 16; ++i)
 #pragma unroll
-            for (int j = 0; j < FJ; ++j)
-#pragma unroll
-                for (int r = 0; r < MF * MF / 64; r += 4) {  // four columns of the row that the lane has
-                    const Sums& all = sum[round * ROUND / MF + i][j];
-                    f32x4 z = {all[r], all[r + 1], all[r + 2], all[r + 3]};
-                    if constexpr (F32) {
-                        z *= kUnscale;
-                        probe += fabsf(z[0]) + fabsf(z[1]) + (fabsf(z[2]) + fabsf(z[3]));
-                    }
-                    *reinterpret_cast<f32x4*>(out + (MF * i + lane % MF) * PITCH + MF * j + 256 / MF * (r / 4) + 4 * (lane / MF)) = z;
+            for (int j = 0; j < FJ; ++j) {  // a lane has four columns of a row
+                f32x4 z = sum[round * ROUND / 16 + i][j];
+                if constexpr (F32) {
+                    z *= kUnscale;
+                    probe += fabsf(z[0]) + fabsf(z[1]) + (fabsf(z[2]) + fabsf(z[3]));
                 }
+                *reinterpret_cast<f32x4*>(out + (16 * i + lane % 16) * PITCH + 16 * j + 4 * (lane / 16)) = z;
+            }
         if constexpr (F32)
             // sums that are not finite are formed again: an infinite value has no parts
             if (splits == 1 && __any(!is_finite(probe))) {
@@ -418,8 +415,20 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
                     if (i < a.I && j < a.J && !is_finite(z)) z = chain(a, i, j);
                 }
             }
+        if (added && col + VEC <= a.J) {
+#pragma unroll
+            for (int r = 0; r < PER; ++r) {
+                float z[VEC];
+                load_values(out + (r * STEP + lane / LANES) * PITCH + lane % LANES * VEC, z);
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) z[c] += bias[c] + (float)residual[round * PER + r][c];
+                const int64_t row = i0 + wi + round * ROUND + r * STEP + lane / LANES;
+                if (row < a.I) store_values(static_cast<T*>(a.e.Y) + row * a.e.ldy + col, z);
+            }
+            continue;
+        }
 #pragma unroll 1
-        for (int b = 0; b < ROUND / STEP; b += BATCH) {
+        for (int b = 0; b < PER; b += BATCH) {
             float z[BATCH][VEC];
             int64_t row[BATCH];
             const int first = b * STEP + lane / LANES, in_rows = wi + round * ROUND + first;
@@ -470,14 +479,14 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a) {
 }
 
 // a: whole = how many tiles not to share; i_tiles and j_tiles are set here.
-template <class T, int TI, int TJ, int WI, int WJ, int MF, int DEPTH, int STAGES, bool A_K, bool B_K>
+template <class T, int TI, int TJ, int WI, int WJ, int DEPTH, int STAGES, bool A_K, bool B_K>
 hipError_t launch(ProductArgs a, hipStream_t s) {
     const int64_t i_tiles = (a.I + TI - 1) / TI, j_tiles = (a.J + TJ - 1) / TJ, tiles = i_tiles * j_tiles;
     if (tiles > (1 << 30) || (tiles - a.whole) * a.splits > (1 << 30)) return hipErrorInvalidValue;
     a.i_tiles = (int)i_tiles, a.j_tiles = (int)j_tiles;
     const int shared = (int)tiles - a.whole;
     const unsigned blocks = (a.whole + 7) / 8 * 8 + (shared * a.splits + 7) / 8 * 8;
-    hipLaunchKernelGGL((product_kernel<T, TI, TJ, WI, WJ, MF, DEPTH, STAGES, A_K, B_K>), dim3(blocks), dim3(64 * WI * WJ), 0, s, a);
+    hipLaunchKernelGGL((product_kernel<T, TI, TJ, WI, WJ, DEPTH, STAGES, A_K, B_K>), dim3(blocks), dim3(64 * WI * WJ), 0, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || shared == 0 || a.splits == 1) return e;
     const int64_t quads = (int64_t)shared * TI * TJ / 4;
     hipLaunchKernelGGL((join_kernel<T, TI, TJ>), dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 1 << 16)), dim3(256), 0, s, a);
@@ -491,18 +500,18 @@ hipError_t launch_tile(int tile, bool a_k, bool b_k, const ProductArgs& a, hipSt
         constexpr bool AK = decltype(ak)::value, BK = decltype(bk)::value;
         if constexpr (sizeof(T) == 4) {
             switch (tile) {
-                case 0: return launch<T, 128, 256, 2, 4, 16, 32, 2, AK, BK>(a, s);
-                case 1: return launch<T, 128, 128, 2, 4, 16, 32, 2, AK, BK>(a, s);
-                case 2: return launch<T, 64, 128, 2, 2, 16, 32, 2, AK, BK>(a, s);
-                default: return launch<T, 64, 64, 2, 2, 16, 32, 2, AK, BK>(a, s);
+                case 0: return launch<T, 128, 256, 2, 4, 32, 2, AK, BK>(a, s);
+                case 1: return launch<T, 128, 128, 2, 4, 32, 2, AK, BK>(a, s);
+                case 2: return launch<T, 64, 128, 2, 2, 32, 2, AK, BK>(a, s);
+                default: return launch<T, 64, 64, 2, 2, 32, 2, AK, BK>(a, s);
             }
         } else {
             switch (tile) {
-                case 0: return launch<T, 256, 256, 2, 4, 16, 32, 3, AK, BK>(a, s);
-                case 1: return launch<T, 128, 128, 2, 4, 16, 64, 2, AK, BK>(a, s);
-                case 2: return launch<T, 64, 128, 2, 4, 16, 64, 2, AK, BK>(a, s);
-                case 3: return launch<T, 64, 64, 2, 2, 16, 64, 3, AK, BK>(a, s);
-                default: return launch<T, 32, 64, 1, 4, 16, 64, 3, AK, BK>(a, s);
+                case 0: return launch<T, 256, 256, 2, 4, 32, 3, AK, BK>(a, s);
+                case 1: return launch<T, 128, 128, 2, 4, 64, 2, AK, BK>(a, s);
+                case 2: return launch<T, 64, 128, 2, 4, 64, 2, AK, BK>(a, s);
+                case 3: return launch<T, 64, 64, 2, 2, 64, 3, AK, BK>(a, s);
+                default: return launch<T, 32, 64, 1, 4, 64, 3, AK, BK>(a, s);
             }
         }
     };

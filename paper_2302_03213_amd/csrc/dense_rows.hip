@@ -82,79 +82,132 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(const T* __restrict_
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// Four consecutive k of one outer index, zeros from k_left on.
-template <bool K_INNER>
-__device__ __forceinline__ f32x4 four(const PlainOperand& o, int64_t outer, int64_t k, int k_left) {
-    const float* const at = o.p + outer * o.outer + k * o.inner;
-    f32x4 v;
-    if (K_INNER && k_left >= 4) {
-        float x[4];
-        load_values(at, x);
-        return f32x4{x[0], x[1], x[2], x[3]};
-    }
+// F fragments of an operand, 16 F outer indices from `first` on by 16 k: v[e][r] is the value at k + r, k being the lane group's first,
+// and at the outer index that index_of(e, lane % 16) names: lanes read 16 bytes along k, or F neighbours at each k.
+template <int F, bool K_INNER>
+__device__ __forceinline__ int index_of(int e, int i) {
+    return K_INNER ? 16 * e + i : F * i + e;
+}
+template <int F, bool K_INNER>
+__device__ __forceinline__ void load_fragments(const PlainOperand& o, int64_t first, int64_t count, int64_t k, int64_t K, f32x4 (&v)[F]) {
+    const int i = threadIdx.x & 15;
+    if constexpr (K_INNER) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = r < k_left ? at[r * o.inner] : 0.f;
-    return v;
+        for (int e = 0; e < F; ++e) {
+            const float* const at = o.p + min(first + 16 * e + i, count - 1) * o.outer;
+            if (k + 4 <= K) {
+                float x[4];
+                load_values(at + k, x);
+                v[e] = f32x4{x[0], x[1], x[2], x[3]};
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[e][r] = k + r < K ? at[k + r] : 0.f;
+            }
+        }
+    } else {
+        const int64_t outer = first + F * i;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float* const at = o.p + min(k + r, K - 1) * o.inner;
+            float x[F];
+            if (outer + F <= count)
+                load_values(at + outer, x);
+            else
+#pragma unroll
+                for (int e = 0; e < F; ++e) x[e] = at[min(outer + e, count - 1)];
+#pragma unroll
+            for (int e = 0; e < F; ++e) v[e][r] = k + r < K ? x[e] : 0.f;
+        }
+    }
 }
 
-// 16 FI rows by 16 columns per workgroup on the fp32 matrix instructions; the wavefronts take every eighth 16 k, and add up in LDS.
-// An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of both operands, and instruction r takes the
-// r-th of each.  grid: row blocks * strips, row block fastest.
-template <int FI, bool A_K, bool B_K>
+// 16 FI rows by 16 FJ columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth
+// 16 k, two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of
+// both operands, and instruction r takes the r-th of each.  grid: row blocks * column blocks, row block fastest.
+template <int FI, int FJ, bool A_K, bool B_K>
 __global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainOperand A, PlainOperand B, int64_t I, int J, int64_t K, int row_blocks,
-                                                             int strips, Epilogue e) {
-    constexpr int AHEAD = FI == 1 ? 4 : 2;
-    __shared__ float part[kWaves][FI * 16][kCols + 1];
-    const int block = strip_of(blockIdx.x, row_blocks * strips);
+                                                             int col_blocks, Epilogue e) {
+    constexpr int COLS = 16 * FJ;
+    __shared__ float part[kWaves][FI * 16][COLS + 1];
+    const int block = strip_of(blockIdx.x, row_blocks * col_blocks);
     if (block < 0) return;
     const int64_t i0 = (int64_t)(block % row_blocks) * FI * 16;
-    const int j0 = block / row_blocks * kCols;
+    const int j0 = block / row_blocks * COLS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, q = lane >> 4;
-    f32x4 sum[FI] = {};
-    const auto add = [&](auto count, int64_t k0) {
-        constexpr int n = decltype(count)::value;
-        f32x4 a[n][FI], b[n];
-#pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const int64_t k = k0 + u * 16 * kWaves + 4 * q;
-            const int left = (int)max((int64_t)0, min(K - k, (int64_t)4));
-            const int64_t in = min(k, K - 1);
-            b[u] = four<B_K>(B, min(j0 + i16, J - 1), in, left);
-#pragma unroll
-            for (int i = 0; i < FI; ++i) a[u][i] = four<A_K>(A, min(i0 + 16 * i + i16, I - 1), in, left);
-        }
-#pragma unroll
-        for (int u = 0; u < n; ++u)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int i = 0; i < FI; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[u][r], a[u][i][r], sum[i], 0, 0, 0);
+    f32x4 sum[FI][FJ] = {};
+    struct Chunk {
+        f32x4 a[FI], b[FJ];
     };
+    const auto load = [&](Chunk& c, int64_t k) {
+        if (k >= K) return;
+        load_fragments<FJ, B_K>(B, j0, J, k + 4 * q, K, c.b);
+        load_fragments<FI, A_K>(A, i0, I, k + 4 * q, K, c.a);
+    };
+    const auto multiply = [&](const Chunk& c) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(c.b[j][r], c.a[i][r], sum[i][j], 0, 0, 0);
+    };
+    constexpr int STEP = 16 * kWaves;
+    Chunk one, two;
     int64_t k = 16 * wave;
-    for (; k + (AHEAD / 2) * 16 * kWaves < K; k += AHEAD * 16 * kWaves) add(std::integral_constant<int, AHEAD>(), k);
-    if (k < K) add(std::integral_constant<int, AHEAD / 2>(), k);
+    load(one, k);
+    load(two, k + STEP);
+    for (; k < K; k += 2 * STEP) {
+        {
+            const Chunk now = one;
+            load(one, k + 2 * STEP);
+            multiply(now);
+        }
+        if (k + STEP >= K) break;
+        const Chunk now = two;
+        load(two, k + 3 * STEP);
+        multiply(now);
+    }
     // the first operand's index is the instruction's row: a lane has columns 4 q .. 4 q + 3 of row i16
 #pragma unroll
     for (int i = 0; i < FI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) part[wave][16 * i + i16][4 * q + r] = sum[i][r];
+        for (int j = 0; j < FJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) part[wave][index_of<FI, A_K>(i, i16)][index_of<FJ, B_K>(j, 4 * q + r)] = sum[i][j][r];
     __syncthreads();
-    for (int v = threadIdx.x; v < FI * 16 * kCols; v += kThreads) {
-        const int64_t row[1] = {i0 + v / kCols};
-        const int col = j0 + v % kCols;
+    for (int v = threadIdx.x; v < FI * 16 * COLS; v += kThreads) {
+        const int64_t row[1] = {i0 + v / COLS};
+        const int col = j0 + v % COLS;
         if (row[0] >= I || col >= J) continue;
         float z[1][1] = {{0.f}}, bias[1];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) z[0][0] += part[w][v / kCols][v % kCols];
+        for (int w = 0; w < kWaves; ++w) z[0][0] += part[w][v / COLS][v % COLS];
         load_bias(e, col, J, bias);
         finish<float>(e, row, col, I, J, bias, z);
     }
 }
 
-// Row fragments per workgroup: up to four, which read a strip of W once for all of them, but a workgroup for every compute unit first.
-int row_fragments(int64_t I, int J, int units) {
-    const int64_t strips = (J + kCols - 1) / kCols, fragments = (I + 15) / 16;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(4, fragments * strips / units));
+// Fragments of rows and of columns per workgroup, and what a round of workgroups, one per compute unit, takes per k and beside that, in us: the three
+// layouts' average over products of 37 x 768 to 2048 x 2048.  (Four by four spill.)
+struct Block {
+    int fi, fj;
+    float per_k, rest;
+};
+constexpr Block kBlocks[] = {{1, 1, 0.0032f, 0.6f}, {2, 2, 0.0075f, 1.2f}, {4, 2, 0.0128f, 1.8f}};
+
+int64_t blocks_of(const Block& b, int64_t I, int J) { return ((I + 16 * b.fi - 1) / (16 * b.fi)) * ((J + 16 * b.fj - 1) / (16 * b.fj)); }
+
+// A launch, and rounds of workgroups.
+float block_us(const Block& b, int64_t I, int J, int64_t K, int units) {
+    return 3.f + (float)((blocks_of(b, I, J) + units - 1) / units) * (K * b.per_k + b.rest);
+}
+
+int best_block(int64_t I, int J, int64_t K) {
+    const int units = compute_units();
+    int best = 0;
+    for (int i = 1; i < (int)(sizeof(kBlocks) / sizeof(kBlocks[0])); ++i)
+        if (block_us(kBlocks[i], I, J, K, units) < block_us(kBlocks[best], I, J, K, units)) best = i;
+    return best;
 }
 
 }  // namespace
@@ -175,32 +228,27 @@ hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, con
 }
 
 hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_t I, int J, int64_t K, const Epilogue& e, hipStream_t s) {
-    const int fragments = row_fragments(I, J, compute_units()), strips = (J + kCols - 1) / kCols;
-    const int64_t row_blocks = (I + 16 * fragments - 1) / (16 * fragments);
-    if (row_blocks * strips > (1 << 30)) return hipErrorInvalidValue;
-    const auto with = [&](auto fi) {
+    const auto with = [&](auto fi, auto fj) {
+        constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
+        const int64_t row_blocks = (I + 16 * FI - 1) / (16 * FI), col_blocks = (J + 16 * FJ - 1) / (16 * FJ);
+        if (row_blocks * col_blocks > (1 << 30)) return hipErrorInvalidValue;
         const auto launch = [&](auto ak, auto bk) {
-            hipLaunchKernelGGL((plain_f32_kernel<decltype(fi)::value, decltype(ak)::value, decltype(bk)::value>),
-                               dim3((unsigned)(row_blocks * strips + 7) / 8 * 8), dim3(kThreads), 0, s, A, B, I, J, K, (int)row_blocks,
-                               strips, e);
+            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, decltype(ak)::value, decltype(bk)::value>),
+                               dim3((unsigned)(row_blocks * col_blocks + 7) / 8 * 8), dim3(kThreads), 0, s, A, B, I, J, K, (int)row_blocks,
+                               (int)col_blocks, e);
             return hipGetLastError();
         };
         if (A.inner != 1) return launch(std::false_type(), std::false_type());
         return B.inner == 1 ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
     };
-    switch (fragments) {
-        case 1: return with(std::integral_constant<int, 1>());
-        case 2: return with(std::integral_constant<int, 2>());
-        case 3: return with(std::integral_constant<int, 3>());
-        default: return with(std::integral_constant<int, 4>());
+    using std::integral_constant;
+    switch (best_block(I, J, K)) {
+        case 0: return with(integral_constant<int, 1>(), integral_constant<int, 1>());
+        case 1: return with(integral_constant<int, 2>(), integral_constant<int, 2>());
+        default: return with(integral_constant<int, 4>(), integral_constant<int, 2>());
     }
 }
 
-// A launch, and 2.3 ns per k, fragment and round of workgroups.
-float plain_f32_us(int64_t I, int J, int64_t K) {
-    const int units = compute_units(), fragments = row_fragments(I, J, units);
-    const int64_t blocks = ((I + 16 * fragments - 1) / (16 * fragments)) * ((J + kCols - 1) / kCols);
-    return 4.f + (float)((blocks + units - 1) / units) * K * 0.0023f * (fragments + 0.25f);
-}
+float plain_f32_us(int64_t I, int J, int64_t K) { return block_us(kBlocks[best_block(I, J, K)], I, J, K, compute_units()); }
 
 }  // namespace lutnn
