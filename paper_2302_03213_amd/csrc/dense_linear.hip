@@ -69,11 +69,12 @@ struct LayOut {
     uint16_t* to[2];
 };
 
+// By workgroup `block` of `blocks` of 256 threads.
 template <class T>
-__global__ __launch_bounds__(256) void lay_out_kernel(LayOut a) {
+__device__ __forceinline__ void lay_out_matrices(const LayOut& a, int block, int blocks) {
     int64_t units[2];
     for (int m = 0; m < 2; ++m) units[m] = a.to[m] ? a.rows[m] * (laid_out_units(a.width[m])) : 0;
-    for (int64_t v = blockIdx.x * 256LL + threadIdx.x; v < units[0] + units[1]; v += gridDim.x * 256LL) {
+    for (int64_t v = block * 256LL + threadIdx.x; v < units[0] + units[1]; v += blocks * 256LL) {
         const int m = v >= units[0];
         const int64_t u = m ? v - units[0] : v, per_row = laid_out_units(a.width[m]);
         const int64_t row = u / per_row, col = (u - row * per_row) * kVec;
@@ -81,6 +82,11 @@ __global__ __launch_bounds__(256) void lay_out_kernel(LayOut a) {
         load_row(static_cast<const T*>(a.from[m]) + row * a.ld[m], col, a.width[m], x);
         lay_out<T>(x, a.to[m] + u * kVec, a.rows[m] * per_row * kVec);
     }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void lay_out_kernel(LayOut a) {
+    lay_out_matrices<T>(a, blockIdx.x, gridDim.x);
 }
 
 struct SlopeArgs {
@@ -94,10 +100,12 @@ struct SlopeArgs {
 };
 
 // dZ = G act'(Z), laid out, and its column sums.  A workgroup takes 8 * lanes columns and every chunks-th group of rows; a thread
-// keeps its eight columns.  grid: chunks * col_tiles, column tile fastest.
+// keeps its eight columns.  grid: chunks * col_tiles, column tile fastest; those behind them lay X and W out.
 template <class T>
-__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, LayOut others) {
     __shared__ float part[256][kVec + 1];
+    const int own = a.chunks * a.col_tiles;
+    if ((int)blockIdx.x >= own) return lay_out_matrices<T>(others, blockIdx.x - own, gridDim.x - own);
     const int sub = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes, rows = 256 / a.lanes;
     const int64_t col = ((int64_t)(blockIdx.x % a.col_tiles) * a.lanes + lane) * kVec;
     const int chunk = blockIdx.x / a.col_tiles;
@@ -214,7 +222,7 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows) {
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
         const float stage = t.depth / 64.f * (dtype == 0 && k_rows == 2 ? t.by_rows : 1.f);
         const float us = kLaunchUs + tiles_us(t, (float)tiles, k_tiles * stage, (float)units);
-        if (us < best.us) best = {i, (int)std::min<int64_t>(tiles, 1 << 30), 1, tiles, us};
+        if (us < best.us) best = {i, (int)std::min<int64_t>(tiles, 1 << 29), 1, tiles, us};
         const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
         const float base = kLaunchUs + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
         if (shared == 0) continue;
@@ -228,31 +236,85 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows) {
     return best;
 }
 
-size_t partial_bytes(int dtype, const Plan& p) {
-    const TileSize& t = dtype == 0 ? kTilesF32[p.tile] : kTiles16[p.tile];
-    return p.splits > 1 ? (size_t)p.splits * (p.tiles - p.whole) * t.i * t.j * 4 : 0;
+// Both gradients' products in one launch: of one tile, and every sum of a product shared out or none.
+struct PairPlan {
+    int tile, x_splits, w_splits, x_first;
+    int64_t x_tiles, w_tiles;
+    float us;
+};
+
+PairPlan pair_plan(int dtype, int64_t N, int D, int M) {
+    const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
+    const int count = dtype == 0 ? 4 : 5;
+    const float units = (float)compute_units();
+    PairPlan best = {0, 1, 1, 0, 0, 0, 1e30f};
+    for (int i = 0; i < count; ++i) {
+        const TileSize& t = sizes[i];
+        const int64_t x_tiles = ((N + t.i - 1) / t.i) * ((D + t.j - 1) / t.j), w_tiles = ((int64_t)(D + t.i - 1) / t.i) * ((M + t.j - 1) / t.j);
+        const float x_stages = (float)((M + t.depth - 1) / t.depth), w_stages = (float)((N + t.depth - 1) / t.depth);
+        const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / kBytesPerUs;
+        for (const int xs : {1, 2, 4}) {
+            if (xs > 1 && (xs > x_stages || x_tiles > slots)) break;
+            for (const int ws : {1, 2, 4, 8, 16, 32}) {
+                if (ws > 1 && (ws > w_stages || w_tiles * ws > 4 * slots)) break;
+                const float nx = (float)x_tiles * xs, nw = (float)w_tiles * ws;
+                const float kx = std::ceil(x_stages / xs) * unit * t.by_rows, kw = std::ceil(w_stages / ws) * unit;
+                // alone as many at once as there are; else the work by the slots, and half the longer tile for the end
+                const int at_once = std::min((int)std::ceil((nx + nw) / units), t.at_once) - 1;
+                const float x = kx * t.stage[at_once] + t.rest[at_once], w = kw * t.stage[at_once] + t.rest[at_once];
+                float us = std::max(x, w);
+                if (nx + nw > slots) us = std::max(us, (nx * x + nw * w) / slots + 0.4f * std::max(x, w));
+                us += kLaunchUs + (xs > 1 ? kJoinUs + nx * tile_bytes : 0.f) + (ws > 1 ? kJoinUs + nw * tile_bytes : 0.f);
+                if (us < best.us) best = {i, xs, ws, x >= w, x_tiles, w_tiles, us};
+            }
+        }
+    }
+    return best;
 }
+
+size_t tile_bytes(int dtype, int tile, int64_t tiles, int splits) {
+    const TileSize& t = dtype == 0 ? kTilesF32[tile] : kTiles16[tile];
+    return splits > 1 ? (size_t)splits * tiles * t.i * t.j * 4 : 0;
+}
+
+size_t partial_bytes(int dtype, const Plan& p) { return tile_bytes(dtype, p.tile, p.tiles - p.whole, p.splits); }
 
 // Laying `values` fp32 values out: read, and written as three parts.
 float lay_out_us(float values) { return kLaunchUs + values * 10 / kBytesPerUs; }
 
-hipError_t run(int dtype, const Plan& p, bool a_k, bool b_k, const Operand& A, const Operand& B, int64_t I, int J, int64_t K, void* partial,
-               const Epilogue& e, hipStream_t s) {
-    ProductArgs a = {A, B, I, K, J, 0, 0, p.whole, p.splits, static_cast<float*>(partial), e};
+ProductArgs product_args(const Operand& A, const Operand& B, int64_t I, int J, int64_t K, int whole, int splits, void* partial,
+                         const Epilogue& e) {
+    return {A, B, I, K, J, 0, 0, whole, splits, static_cast<float*>(partial), e};
+}
+
+hipError_t run(int dtype, int tile, bool a_k, bool b_k, const ProductArgs& a, hipStream_t s) {
     switch (dtype) {
-        case 0: return launch_product_f32(p.tile, a_k, b_k, a, s);
-        case 1: return launch_product_bf16(p.tile, a_k, b_k, a, s);
-        default: return launch_product_f16(p.tile, a_k, b_k, a, s);
+        case 0: return launch_product_f32(tile, a_k, b_k, a, s);
+        case 1: return launch_product_bf16(tile, a_k, b_k, a, s);
+        default: return launch_product_f16(tile, a_k, b_k, a, s);
     }
 }
 
-hipError_t lay_out_matrices(int dtype, const LayOut& a, hipStream_t s) {
+hipError_t run(int dtype, int tile, const PairArgs& p, hipStream_t s) {
+    switch (dtype) {
+        case 0: return launch_pair_f32(tile, p, s);
+        case 1: return launch_pair_bf16(tile, p, s);
+        default: return launch_pair_f16(tile, p, s);
+    }
+}
+
+unsigned lay_out_blocks(const LayOut& a) {
     int64_t units = 0;
     for (int m = 0; m < 2; ++m)
         if (a.to[m]) units += a.rows[m] * (laid_out_stride(a.width[m]) / kVec);
-    if (units == 0) return hipSuccess;
+    return (unsigned)std::min<int64_t>((units + 255) / 256, 1 << 15);
+}
+
+hipError_t launch_lay_out(int dtype, const LayOut& a, hipStream_t s) {
+    const unsigned blocks = lay_out_blocks(a);
+    if (blocks == 0) return hipSuccess;
     return with_type(dtype, [&](auto t) {
-        hipLaunchKernelGGL(lay_out_kernel<decltype(t)>, dim3((unsigned)std::min<int64_t>((units + 255) / 256, 1 << 15)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(lay_out_kernel<decltype(t)>, dim3(blocks), dim3(256), 0, s, a);
         return hipGetLastError();
     });
 }
@@ -275,26 +337,32 @@ Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t
     return o;
 }
 
-// What the backward pass has to have laid out, and its products.
+// What the backward pass has to have laid out, and its products: of both gradients in one launch, or of one.
 struct GradientPlan {
     bool plain;  // fp32 products of the operands as they are
-    bool x, w, z, sums, pass;
-    Plan to_x, to_w;
+    bool x, w, z, sums, pass, both;
+    Plan one;
+    PairPlan pair;
     SlopeArgs slope;
-    size_t partial;
+    size_t x_partial, partial;
 };
 
 GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int activation, bool need_dx, bool need_dw, bool need_db) {
     GradientPlan g = {};
-    float tiles = 0.f, plain = 0.f, values = (float)c.N * c.M;
-    if (need_dx) {
-        g.to_x = plan(c.dtype, c.N, c.D, c.M, 2);
-        tiles += g.to_x.us, plain += plain_f32_us(c.N, c.D, c.M), values += (float)c.D * c.M;
+    g.both = need_dx && need_dw;
+    float tiles = 0.f, plain = 0.f;
+    const float values = (float)c.N * c.M + (need_dx ? (float)c.D * c.M : 0.f) + (need_dw ? (float)c.N * c.D : 0.f);
+    if (g.both) {
+        g.pair = pair_plan(c.dtype, c.N, c.D, c.M);
+        tiles = g.pair.us, plain = plain_pair_us(c.N, c.D, c.M);
+    } else if (need_dx) {
+        g.one = plan(c.dtype, c.N, c.D, c.M, 2);
+        tiles = g.one.us, plain = plain_f32_us(c.N, c.D, c.M);
+    } else if (need_dw) {
+        g.one = plan(c.dtype, c.D, c.M, c.N, 0);
+        tiles = g.one.us, plain = plain_f32_us(c.D, c.M, c.N);
     }
-    if (need_dw) {
-        g.to_w = plan(c.dtype, c.D, c.M, c.N, 0);
-        tiles += g.to_w.us, plain += plain_f32_us(c.D, c.M, c.N), values += (float)c.N * c.D;
-    }
+    // the pass over G is there for an activation or a bias either way; planes are half as much again to write
     g.plain = c.dtype == 0 && plain < tiles + lay_out_us(values);
     g.x = !g.plain && need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
     g.w = !g.plain && need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
@@ -302,7 +370,12 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     g.sums = need_db;
     g.pass = g.z || g.sums;
     share_rows(c.N, c.M, g.slope);
-    if (!g.plain) g.partial = std::max(need_dx ? partial_bytes(c.dtype, g.to_x) : 0, need_dw ? partial_bytes(c.dtype, g.to_w) : 0);
+    if (!g.plain && g.both) {
+        g.x_partial = tile_bytes(c.dtype, g.pair.tile, g.pair.x_tiles, g.pair.x_splits);
+        g.partial = g.x_partial + tile_bytes(c.dtype, g.pair.tile, g.pair.w_tiles, g.pair.w_splits);
+    } else if (!g.plain && (need_dx || need_dw)) {
+        g.partial = partial_bytes(c.dtype, g.one);
+    }
     return g;
 }
 
@@ -352,10 +425,12 @@ hipError_t launch_dense_linear(const DenseCall& c, const float* bias, int activa
     uint16_t *x = nullptr, *w = nullptr;
     if (f.x) x = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.N, c.D)));
     if (f.w) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
-    if (hipError_t e = lay_out_matrices(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
+    if (hipError_t e = launch_lay_out(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
     const bool f32 = c.dtype == 0;
-    return run(c.dtype, f.product, true, false, operand(c.X, c.ldx, x, c.N, c.D, true, f32), operand(c.W, c.ldw, w, c.D, c.M, false, f32),
-               c.N, c.M, c.D, shares.take(0), epilogue, s);
+    return run(c.dtype, f.product.tile, true, false,
+               product_args(operand(c.X, c.ldx, x, c.N, c.D, true, f32), operand(c.W, c.ldw, w, c.D, c.M, false, f32), c.N, c.M, c.D,
+                            f.product.whole, f.product.splits, shares.take(0), epilogue),
+               s);
 }
 
 size_t dense_linear_gradient_workspace(const DenseCall& c, const void* G, int64_t ldg, const void*, int64_t, int activation,
@@ -376,28 +451,33 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     if (g.w) w = static_cast<uint16_t*>(shares.take(laid_out_bytes(c.dtype, c.D, c.M)));
     if (g.z) z = static_cast<uint16_t*>(shares.take(slope_bytes(c, g)));
     float* const columns = static_cast<float*>(shares.take(column_bytes(g, c.M)));
-    if (hipError_t e = lay_out_matrices(c.dtype, {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}}, s)) return e;
+    float *const x_partial = static_cast<float*>(shares.take(g.x_partial)), *const w_partial = static_cast<float*>(shares.take(0));
+    const LayOut others = {{c.X, c.W}, {c.ldx, c.ldw}, {c.N, c.D}, {c.D, c.M}, {x, w}};
     if (g.pass) {
         SlopeArgs& a = g.slope;
         a.G = G, a.Z = Z, a.ldg = ldg, a.ldz = ldz, a.N = c.N, a.M = c.M, a.activation = activation;
         a.to = z, a.plain = g.plain, a.partial = db ? columns : nullptr;
         const hipError_t e = with_type(c.dtype, [&](auto t) {
-            hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles)), dim3(256), 0, s, a);
+            hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles) + lay_out_blocks(others)), dim3(256), 0, s,
+                               a, others);
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
-        if (db)
-            if (hipError_t e = launch_partial_sums(columns, a.chunks, c.M, c.M, db, nullptr, s)) return e;
+    } else if (hipError_t e = launch_lay_out(c.dtype, others, s)) {
+        return e;
     }
+    const PartialSums sums = {columns, g.slope.chunks, c.M, db};
+    if (!g.both && db)
+        if (hipError_t e = launch_partial_sums(columns, g.slope.chunks, c.M, c.M, db, nullptr, s)) return e;
+    if (!dX && !dW) return hipSuccess;
+    const Epilogue to_x = {nullptr, 0, nullptr, dX, nullptr, 0, lddx, 0}, to_w = {nullptr, 0, nullptr, dW, nullptr, 0, lddw, 0};
     if (g.plain) {
-        const float *const dz = static_cast<const float*>(g.z ? static_cast<const void*>(z) : G), *const X = static_cast<const float*>(c.X);
+        const float *const dz = static_cast<const float*>(g.z ? static_cast<const void*>(z) : G), *const X = static_cast<const float*>(c.X),
+                    *const W = static_cast<const float*>(c.W);
         const int64_t ld = g.z ? c.M : ldg;
-        if (dX)
-            if (hipError_t e = launch_plain_f32({dz, ld, 1}, {static_cast<const float*>(c.W), c.ldw, 1}, c.N, c.D, c.M,
-                                                {nullptr, 0, nullptr, dX, nullptr, 0, lddx, 0}, s))
-                return e;
-        return !dW ? hipSuccess
-                   : launch_plain_f32({X, 1, c.ldx}, {dz, 1, ld}, c.D, c.M, c.N, {nullptr, 0, nullptr, dW, nullptr, 0, lddw, 0}, s);
+        if (g.both) return launch_plain_pair_f32(dz, ld, W, c.ldw, X, c.ldx, c.N, c.D, c.M, to_x, to_w, sums, s);
+        return dX ? launch_plain_f32({dz, ld, 1}, {W, c.ldw, 1}, c.N, c.D, c.M, to_x, s)
+                  : launch_plain_f32({X, 1, c.ldx}, {dz, 1, ld}, c.D, c.M, c.N, to_w, s);
     }
     const bool f32 = c.dtype == 0;
     const auto gradient = [&](bool k_inner) {
@@ -408,14 +488,16 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
         }
         return o;
     };
-    void* const partial = shares.take(0);
-    if (dX)
-        if (hipError_t e = run(c.dtype, g.to_x, true, true, gradient(true), operand(c.W, c.ldw, w, c.D, c.M, true, f32), c.N, c.D, c.M,
-                               partial, {nullptr, 0, nullptr, dX, nullptr, 0, lddx, 0}, s))
-            return e;
-    if (!dW) return hipSuccess;
-    return run(c.dtype, g.to_w, false, false, operand(c.X, c.ldx, x, c.N, c.D, false, f32), gradient(false), c.D, c.M, c.N, partial,
-               {nullptr, 0, nullptr, dW, nullptr, 0, lddw, 0}, s);
+    const auto product = [&](bool of_x, int whole, int splits, float* partial) {
+        return of_x ? product_args(gradient(true), operand(c.W, c.ldw, w, c.D, c.M, true, f32), c.N, c.D, c.M, whole, splits, partial, to_x)
+                    : product_args(operand(c.X, c.ldx, x, c.N, c.D, false, f32), gradient(false), c.D, c.M, c.N, whole, splits, partial, to_w);
+    };
+    if (!g.both) return run(c.dtype, g.one.tile, dX != nullptr, dX != nullptr, product(dX, g.one.whole, g.one.splits, w_partial), s);
+    const PairPlan& p = g.pair;
+    return run(c.dtype, p.tile,
+               {product(true, p.x_splits > 1 ? 0 : (int)p.x_tiles, p.x_splits, x_partial),
+                product(false, p.w_splits > 1 ? 0 : (int)p.w_tiles, p.w_splits, w_partial), 0, 0, p.x_first, sums},
+               s);
 }
 
 }  // namespace lutnn

@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "dense_epilogue.h"
+#include "dense_rows.h"
 #include "lutnn_kernels.h"
 #include "mfma_tile.h"
 #include "split_bf16.h"
@@ -31,6 +32,13 @@ struct ProductArgs {
     int whole, splits;  // so many tiles are one workgroup's each; `splits` share the sum of each of the others
     float* partial;     // theirs: [splits][tiles - whole][rows of a tile][columns of it]
     Epilogue e;
+};
+
+// Both gradients' products in one launch (product::pair_kernel).
+struct PairArgs {
+    ProductArgs x, w;
+    int x_blocks, w_blocks, x_first;  // the blocks are counted at the launch
+    PartialSums sums;
 };
 
 namespace product {
@@ -199,24 +207,34 @@ __device__ __forceinline__ void interleave() {
     }
 }
 
-// One tile per workgroup.  T: the matrices' type; fp32 ones are PARTS = 3 planes of bf16 (split_bf16.h).  WI x WJ wavefronts.
-template <class T, int TI, int TJ, int WI, int WJ, int DEPTH, int STAGES, bool A_K, bool B_K>
-__global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
-    constexpr bool F32 = sizeof(T) == 4;
-    constexpr int PARTS = F32 ? 3 : 1, THREADS = 64 * WI * WJ;
-    constexpr int FI = TI / WI / 16, FJ = TJ / WJ / 16, STEPS = DEPTH / 32;
+// A tile's size, wavefronts and ring.  T: the matrices' type; fp32 ones are three planes of bf16 (split_bf16.h).
+template <class T_, int TI_, int TJ_, int WI_, int WJ_, int DEPTH_, int STAGES_>
+struct Config {
+    typedef T_ T;
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, DEPTH = DEPTH_, STAGES = STAGES_;
+    static constexpr int PARTS = F32 ? 3 : 1, THREADS = 64 * WI * WJ, BUF = (TI + TJ) * DEPTH * 2 * PARTS;
+    // the sums on their way out: a wavefront's, ROUND rows at a time
+    static constexpr int ROUND = TI / WI < 64 ? TI / WI : 64, COLS = TJ / WJ, PITCH = COLS + 4, OUT = WI * WJ * ROUND * PITCH * 4;
+    static constexpr int LDS = STAGES * BUF > OUT ? STAGES * BUF : OUT;
+};
+
+// Workgroup `block`'s tile of a product; lds: C::LDS bytes.
+template <class C, bool A_K, bool B_K>
+__device__ __forceinline__ void product_tile(const ProductArgs& a, int block, char* const lds) {
+    typedef typename C::T T;
+    constexpr bool F32 = C::F32;
+    constexpr int PARTS = C::PARTS, THREADS = C::THREADS, DEPTH = C::DEPTH, STAGES = C::STAGES, TI = C::TI, TJ = C::TJ, WI = C::WI, WJ = C::WJ;
+    constexpr int FI = TI / WI / 16, FJ = TJ / WJ / 16, STEPS = DEPTH / 32, BUF = C::BUF;
+    constexpr int ROUND = C::ROUND, COLS = C::COLS, PITCH = C::PITCH, kBatch = TI * TJ > 128 * 128 ? 4 : 2;
     typedef typename std::conditional<F32, bf16, T>::type E;
     typedef Tile<TI, DEPTH, A_K, PARTS, THREADS> TileA;
     typedef Tile<TJ, DEPTH, B_K, PARTS, THREADS> TileB;
-    constexpr int BUF = TileA::kBytes + TileB::kBytes;
-    constexpr int kBatch = TI * TJ > 128 * 128 ? 4 : 2;
-    // the sums on their way out: a wavefront's, ROUND rows at a time
-    constexpr int ROUND = TI / WI < 64 ? TI / WI : 64, COLS = TJ / WJ, PITCH = COLS + 4, OUT = WI * WJ * ROUND * PITCH * 4;
-    __shared__ __align__(1024) char lds[STAGES * BUF > OUT ? STAGES * BUF : OUT];
+    static_assert(BUF == TileA::kBytes + TileB::kBytes, "a stage's operands");
 
     const int whole_blocks = (a.whole + 7) / 8 * 8, shared = a.i_tiles * a.j_tiles - a.whole;
-    const bool is_whole = (int)blockIdx.x < whole_blocks;
-    int tile = is_whole ? of_xcd(blockIdx.x, a.whole) : of_xcd(blockIdx.x - whole_blocks, shared * a.splits);
+    const bool is_whole = block < whole_blocks;
+    int tile = is_whole ? of_xcd(block, a.whole) : of_xcd(block - whole_blocks, shared * a.splits);
     if (tile < 0) return;
     const int splits = is_whole ? 1 : a.splits, split = is_whole ? 0 : tile / shared, in_shared = is_whole ? 0 : tile % shared;
     if (!is_whole) tile = a.whole + in_shared;
@@ -376,18 +394,20 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
     const int in_cols = wj + lane % LANES * VEC, col = j0 + in_cols;
     float bias[VEC];
     load_bias(a.e, col, a.J, bias);
-    // A residual without an activation, in whole units: all of it is asked for at once, into registers that held operands.  Batch by
-    // batch each would wait for its own.
+    // A residual without an activation, in whole units: a round's rows are asked for at once and a round ahead, into registers that
+    // held operands and sums.  Batch by batch each would wait for its own.
     constexpr int PER = ROUND / STEP, ROUNDS = TI / WI / ROUND;
-    const bool added = splits == 1 && a.e.R && a.e.activation == kActNone && !a.e.Z;
-    typename Packed<T, VEC>::type residual[ROUNDS * PER];
-    if (added)
+    const bool added = splits == 1 && a.e.R && a.e.activation == kActNone && !a.e.Z && col + VEC <= a.J;
+    typename Packed<T, VEC>::type residual[ROUNDS][PER];
+    const auto fetch = [&](int round) {
+        if (!added) return;
 #pragma unroll
-        for (int r = 0; r < ROUNDS * PER; ++r) {
-            const int64_t row = min(i0 + wi + r * STEP + lane / LANES, a.I - 1);
-            const T* const from = static_cast<const T*>(a.e.R) + row * a.e.ldr + col;
-            if (col + VEC <= a.J) residual[r] = *reinterpret_cast<const typename Packed<T, VEC>::type*>(from);
+        for (int r = 0; r < PER; ++r) {
+            const int64_t row = min(i0 + wi + round * ROUND + r * STEP + lane / LANES, a.I - 1);
+            residual[round][r] = *reinterpret_cast<const typename Packed<T, VEC>::type*>(static_cast<const T*>(a.e.R) + row * a.e.ldr + col);
         }
+    };
+    fetch(0);
     lds_barrier();
     float* const out = reinterpret_cast<float*>(lds) + wave * ROUND * PITCH;
 #pragma unroll
@@ -415,13 +435,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
                     if (i < a.I && j < a.J && !is_finite(z)) z = chain(a, i, j);
                 }
             }
-        if (added && col + VEC <= a.J) {
+        if (round + 1 < ROUNDS) fetch(round + 1);
+        if (added) {
 #pragma unroll
             for (int r = 0; r < PER; ++r) {
                 float z[VEC];
                 load_values(out + (r * STEP + lane / LANES) * PITCH + lane % LANES * VEC, z);
 #pragma unroll
-                for (int c = 0; c < VEC; ++c) z[c] += bias[c] + (float)residual[round * PER + r][c];
+                for (int c = 0; c < VEC; ++c) z[c] += bias[c] + (float)residual[round][r][c];
                 const int64_t row = i0 + wi + round * ROUND + r * STEP + lane / LANES;
                 if (row < a.I) store_values(static_cast<T*>(a.e.Y) + row * a.e.ldy + col, z);
             }
@@ -447,6 +468,25 @@ __global__ __launch_bounds__(64 * WI * WJ) void product_kernel(ProductArgs a) {
             finish<T>(a.e, row, col, a.I, a.J, bias, z);
         }
     }
+}
+
+template <class C, bool A_K, bool B_K>
+__global__ __launch_bounds__(C::THREADS) void product_kernel(ProductArgs a) {
+    __shared__ __align__(1024) char lds[C::LDS];
+    product_tile<C, A_K, B_K>(a, blockIdx.x, lds);
+}
+
+// dX = dZ W^T and dW = X^T dZ in one launch, that with the longer tiles first, and db's partial sums added up beside them.
+template <class C>
+__global__ __launch_bounds__(C::THREADS) void pair_kernel(PairArgs p) {
+    __shared__ __align__(1024) char lds[C::LDS];
+    const int first = p.x_first ? p.x_blocks : p.w_blocks, both = p.x_blocks + p.w_blocks, b = blockIdx.x;
+    if (b >= both)
+        add_partial_sums<C::THREADS>(p.sums, b - both, lds);
+    else if ((b < first) == (p.x_first != 0))
+        product_tile<C, true, true>(p.x, b < first ? b : b - first, lds);
+    else
+        product_tile<C, false, false>(p.w, b < first ? b : b - first, lds);
 }
 
 // The shared tiles' sums through the epilogue, four columns per thread.  TI x TJ: a tile.
@@ -478,53 +518,93 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a) {
     }
 }
 
-// a: whole = how many tiles not to share; i_tiles and j_tiles are set here.
-template <class T, int TI, int TJ, int WI, int WJ, int DEPTH, int STAGES, bool A_K, bool B_K>
-hipError_t launch(ProductArgs a, hipStream_t s) {
-    const int64_t i_tiles = (a.I + TI - 1) / TI, j_tiles = (a.J + TJ - 1) / TJ, tiles = i_tiles * j_tiles;
-    if (tiles > (1 << 30) || (tiles - a.whole) * a.splits > (1 << 30)) return hipErrorInvalidValue;
+inline unsigned blocks_of(const ProductArgs& a) {
+    const int shared = a.i_tiles * a.j_tiles - a.whole;
+    return (a.whole + 7) / 8 * 8 + (shared * a.splits + 7) / 8 * 8;
+}
+
+// Sets i_tiles and j_tiles; false for more tiles than a grid has.
+template <class C>
+bool count_tiles(ProductArgs& a) {
+    const int64_t i_tiles = (a.I + C::TI - 1) / C::TI, j_tiles = (a.J + C::TJ - 1) / C::TJ, tiles = i_tiles * j_tiles;
+    if (tiles > (1 << 29) || (tiles - a.whole) * a.splits > (1 << 29)) return false;
     a.i_tiles = (int)i_tiles, a.j_tiles = (int)j_tiles;
-    const int shared = (int)tiles - a.whole;
-    const unsigned blocks = (a.whole + 7) / 8 * 8 + (shared * a.splits + 7) / 8 * 8;
-    hipLaunchKernelGGL((product_kernel<T, TI, TJ, WI, WJ, DEPTH, STAGES, A_K, B_K>), dim3(blocks), dim3(64 * WI * WJ), 0, s, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || shared == 0 || a.splits == 1) return e;
-    const int64_t quads = (int64_t)shared * TI * TJ / 4;
-    hipLaunchKernelGGL((join_kernel<T, TI, TJ>), dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 1 << 16)), dim3(256), 0, s, a);
+    return true;
+}
+
+template <class C>
+hipError_t join(const ProductArgs& a, hipStream_t s) {
+    const int64_t shared = a.i_tiles * a.j_tiles - a.whole, quads = shared * C::TI * C::TJ / 4;
+    if (shared == 0 || a.splits == 1) return hipSuccess;
+    hipLaunchKernelGGL((join_kernel<typename C::T, C::TI, C::TJ>), dim3((unsigned)std::min<int64_t>((quads + 255) / 256, 1 << 16)), dim3(256),
+                       0, s, a);
     return hipGetLastError();
 }
 
-// The tiles of dense_linear.hip's list by number.
+// a.whole: how many tiles not to share.  A's k is inner but for dW = X^T dZ, B's for dX = dZ W^T.
+template <class C>
+hipError_t launch(ProductArgs a, bool a_k, bool b_k, hipStream_t s) {
+    if (!count_tiles<C>(a)) return hipErrorInvalidValue;
+    const dim3 grid(blocks_of(a)), threads(C::THREADS);
+    if (!a_k)
+        hipLaunchKernelGGL((product_kernel<C, false, false>), grid, threads, 0, s, a);
+    else if (b_k)
+        hipLaunchKernelGGL((product_kernel<C, true, true>), grid, threads, 0, s, a);
+    else
+        hipLaunchKernelGGL((product_kernel<C, true, false>), grid, threads, 0, s, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    return join<C>(a, s);
+}
+
+template <class C>
+hipError_t launch_pair(PairArgs p, hipStream_t s) {
+    if (!count_tiles<C>(p.x) || !count_tiles<C>(p.w)) return hipErrorInvalidValue;
+    p.x_blocks = (int)blocks_of(p.x), p.w_blocks = (int)blocks_of(p.w);
+    const unsigned blocks = p.x_blocks + p.w_blocks + (p.sums.out ? (p.sums.width + 31) / 32 : 0);
+    hipLaunchKernelGGL(pair_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, s, p);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (hipError_t e = join<C>(p.x, s)) return e;
+    return join<C>(p.w, s);
+}
+
+// Calls f with the Config of a tile of dense_linear.hip's lists.
+template <class T, class F>
+hipError_t with_tile(int tile, F&& f) {
+    if constexpr (sizeof(T) == 4) {
+        switch (tile) {
+            case 0: return f(Config<T, 128, 256, 2, 4, 32, 2>());
+            case 1: return f(Config<T, 128, 128, 2, 4, 32, 2>());
+            case 2: return f(Config<T, 64, 128, 2, 2, 32, 2>());
+            default: return f(Config<T, 64, 64, 2, 2, 32, 2>());
+        }
+    } else {
+        switch (tile) {
+            case 0: return f(Config<T, 256, 256, 2, 4, 32, 3>());
+            case 1: return f(Config<T, 128, 128, 2, 4, 64, 2>());
+            case 2: return f(Config<T, 64, 128, 2, 4, 64, 2>());
+            case 3: return f(Config<T, 64, 64, 2, 2, 64, 3>());
+            default: return f(Config<T, 32, 64, 1, 4, 64, 3>());
+        }
+    }
+}
+
 template <class T>
 hipError_t launch_tile(int tile, bool a_k, bool b_k, const ProductArgs& a, hipStream_t s) {
-    const auto with = [&](auto ak, auto bk) {
-        constexpr bool AK = decltype(ak)::value, BK = decltype(bk)::value;
-        if constexpr (sizeof(T) == 4) {
-            switch (tile) {
-                case 0: return launch<T, 128, 256, 2, 4, 32, 2, AK, BK>(a, s);
-                case 1: return launch<T, 128, 128, 2, 4, 32, 2, AK, BK>(a, s);
-                case 2: return launch<T, 64, 128, 2, 2, 32, 2, AK, BK>(a, s);
-                default: return launch<T, 64, 64, 2, 2, 32, 2, AK, BK>(a, s);
-            }
-        } else {
-            switch (tile) {
-                case 0: return launch<T, 256, 256, 2, 4, 32, 3, AK, BK>(a, s);
-                case 1: return launch<T, 128, 128, 2, 4, 64, 2, AK, BK>(a, s);
-                case 2: return launch<T, 64, 128, 2, 4, 64, 2, AK, BK>(a, s);
-                case 3: return launch<T, 64, 64, 2, 2, 64, 3, AK, BK>(a, s);
-                default: return launch<T, 32, 64, 1, 4, 64, 3, AK, BK>(a, s);
-            }
-        }
-    };
-    if (!a_k) return with(std::false_type(), std::false_type());
-    return b_k ? with(std::true_type(), std::true_type()) : with(std::true_type(), std::false_type());
+    return with_tile<T>(tile, [&](auto c) { return launch<decltype(c)>(a, a_k, b_k, s); });
+}
+template <class T>
+hipError_t launch_tiles(int tile, const PairArgs& p, hipStream_t s) {
+    return with_tile<T>(tile, [&](auto c) { return launch_pair<decltype(c)>(p, s); });
 }
 
 }  // namespace product
 
-// dense_product_f32.hip, _bf16.hip, _f16.hip; tile: a size of dense_linear.hip's list.  A's k is inner but for dW = X^T dZ, B's for
-// dX = dZ W^T.
+// dense_product_f32.hip, _bf16.hip, _f16.hip
 hipError_t launch_product_f32(int tile, bool a_k, bool b_k, const ProductArgs& a, hipStream_t s);
 hipError_t launch_product_bf16(int tile, bool a_k, bool b_k, const ProductArgs& a, hipStream_t s);
 hipError_t launch_product_f16(int tile, bool a_k, bool b_k, const ProductArgs& a, hipStream_t s);
+hipError_t launch_pair_f32(int tile, const PairArgs& p, hipStream_t s);
+hipError_t launch_pair_bf16(int tile, const PairArgs& p, hipStream_t s);
+hipError_t launch_pair_f16(int tile, const PairArgs& p, hipStream_t s);
 
 }  // namespace lutnn

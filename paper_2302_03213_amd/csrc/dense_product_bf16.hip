@@ -10,4 +10,6 @@ hipError_t launch_product_bf16(int tile, bool a_k, bool b_k, const ProductArgs& 
     return product::launch_tile<bf16>(tile, a_k, b_k, a, s);
 }
 
+hipError_t launch_pair_bf16(int tile, const PairArgs& p, hipStream_t s) { return product::launch_tiles<bf16>(tile, p, s); }
+
 }  // namespace lutnn

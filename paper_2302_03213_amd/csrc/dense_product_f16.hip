@@ -10,4 +10,6 @@ hipError_t launch_product_f16(int tile, bool a_k, bool b_k, const ProductArgs& a
     return product::launch_tile<f16>(tile, a_k, b_k, a, s);
 }
 
+hipError_t launch_pair_f16(int tile, const PairArgs& p, hipStream_t s) { return product::launch_tiles<f16>(tile, p, s); }
+
 }  // namespace lutnn

@@ -11,6 +11,31 @@ constexpr int kFewRows = 4;
 hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int D, int M,
                            const Epilogue& e, hipStream_t s);
 
+// fp32 sums that a kernel's workgroups left, [count][width], to be added up by workgroups of a later launch; no `out`: none.
+struct PartialSums {
+    const float* partial;
+    int count, width;
+    float* out;
+};
+
+// 32 columns of them by workgroup `block` of THREADS, 64-bit sums in a fixed order.  lds: THREADS / 32 * 33 doubles.
+template <int THREADS>
+__device__ __forceinline__ void add_partial_sums(const PartialSums& p, int block, void* lds) {
+    constexpr int GROUPS = THREADS / 32;
+    double(*const part)[33] = static_cast<double(*)[33]>(lds);
+    const int i = threadIdx.x & 31, group = threadIdx.x >> 5, m = block * 32 + i;
+    double sum = 0;
+    if (m < p.width)
+#pragma unroll 8
+        for (int k = group; k < p.count; k += GROUPS) sum += p.partial[(int64_t)k * p.width + m];
+    part[group][i] = sum;
+    __syncthreads();
+    if (group != 0 || m >= p.width) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) sum += part[k][i];
+    p.out[m] = (float)sum;
+}
+
 // C[i][j] = sum_k A(i, k) B(k, j) of fp32 operands as they are, the value at outer index o and k being p[o * outer + k * inner];
 // one of the two steps is 1.
 struct PlainOperand {
@@ -18,6 +43,11 @@ struct PlainOperand {
     int64_t outer, inner;
 };
 hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_t I, int J, int64_t K, const Epilogue& e, hipStream_t s);
+
+// dX [I][J] and dW [WI][WJ] in one launch, with the partial sums added up beside them: dX = dZ W^T, dW = X^T dZ.
+hipError_t launch_plain_pair_f32(const float* dZ, int64_t ldg, const float* W, int64_t ldw, const float* X, int64_t ldx, int64_t N, int D,
+                                 int M, const Epilogue& to_x, const Epilogue& to_w, const PartialSums& sums, hipStream_t s);
+float plain_pair_us(int64_t N, int D, int M);
 
 // us, as measured
 float plain_f32_us(int64_t I, int J, int64_t K);

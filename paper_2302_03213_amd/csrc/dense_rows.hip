@@ -1,6 +1,7 @@
 // Dense layers of few rows: what bounds them is reading W once and the launch itself, so each is one launch that reads its operands
 // as they are.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "dense_rows.h"
@@ -123,13 +124,26 @@ __device__ __forceinline__ void load_fragments(const PlainOperand& o, int64_t fi
 
 // 16 FI rows by 16 FJ columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth
 // 16 k, two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of
-// both operands, and instruction r takes the r-th of each.  grid: row blocks * column blocks, row block fastest.
+// both operands, and instruction r takes the r-th of each.  Blocks: row blocks * column blocks, row block fastest.
+struct PlainArgs {
+    PlainOperand A, B;
+    int64_t I, K;
+    int J, row_blocks, col_blocks;
+    Epilogue e;
+};
+template <int FI, int FJ>
+struct PlainShared {
+    float part[kWaves][FI * 16][16 * FJ + 1];
+};
 template <int FI, int FJ, bool A_K, bool B_K>
-__global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainOperand A, PlainOperand B, int64_t I, int J, int64_t K, int row_blocks,
-                                                             int col_blocks, Epilogue e) {
+__device__ __forceinline__ void plain_f32_block(const PlainArgs& args, int index, PlainShared<FI, FJ>& shared) {
     constexpr int COLS = 16 * FJ;
-    __shared__ float part[kWaves][FI * 16][COLS + 1];
-    const int block = strip_of(blockIdx.x, row_blocks * col_blocks);
+    auto& part = shared.part;
+    const PlainOperand &A = args.A, &B = args.B;
+    const int64_t I = args.I, K = args.K;
+    const int J = args.J, row_blocks = args.row_blocks;
+    const Epilogue& e = args.e;
+    const int block = strip_of(index, row_blocks * args.col_blocks);
     if (block < 0) return;
     const int64_t i0 = (int64_t)(block % row_blocks) * FI * 16;
     const int j0 = block / row_blocks * COLS;
@@ -187,6 +201,25 @@ __global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainOperand A, Pla
     }
 }
 
+template <int FI, int FJ, bool A_K, bool B_K>
+__global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainArgs a) {
+    __shared__ PlainShared<FI, FJ> shared;
+    plain_f32_block<FI, FJ, A_K, B_K>(a, blockIdx.x, shared);
+}
+
+// Both gradients' products in one launch, and db's partial sums.
+template <int FI, int FJ>
+__global__ __launch_bounds__(kThreads) void plain_pair_kernel(PlainArgs x, PlainArgs w, int x_blocks, int w_blocks, PartialSums sums) {
+    __shared__ __align__(8) PlainShared<FI, FJ> shared;
+    const int b = blockIdx.x;
+    if (b >= x_blocks + w_blocks)
+        add_partial_sums<kThreads>(sums, b - x_blocks - w_blocks, &shared);
+    else if (b < x_blocks)
+        plain_f32_block<FI, FJ, true, true>(x, b, shared);
+    else
+        plain_f32_block<FI, FJ, false, false>(w, b - x_blocks, shared);
+}
+
 // Fragments of rows and of columns per workgroup, and what a round of workgroups, one per compute unit, takes per k and beside that, in us: the three
 // layouts' average over products of 37 x 768 to 2048 x 2048.  (Four by four spill.)
 struct Block {
@@ -195,19 +228,55 @@ struct Block {
 };
 constexpr Block kBlocks[] = {{1, 1, 0.0032f, 0.6f}, {2, 2, 0.0075f, 1.2f}, {4, 2, 0.0128f, 1.8f}};
 
-int64_t blocks_of(const Block& b, int64_t I, int J) { return ((I + 16 * b.fi - 1) / (16 * b.fi)) * ((J + 16 * b.fj - 1) / (16 * b.fj)); }
-
-// A launch, and rounds of workgroups.
-float block_us(const Block& b, int64_t I, int J, int64_t K, int units) {
-    return 3.f + (float)((blocks_of(b, I, J) + units - 1) / units) * (K * b.per_k + b.rest);
+float blocks_of(const Block& b, int64_t I, int J) {
+    return (float)((I + 16 * b.fi - 1) / (16 * b.fi)) * (float)((J + 16 * b.fj - 1) / (16 * b.fj));
 }
 
-int best_block(int64_t I, int J, int64_t K) {
-    const int units = compute_units();
+// A launch, and rounds of workgroups.
+float block_us(const Block& b, int64_t I, int J, int64_t K, float units) {
+    return 3.f + std::ceil(blocks_of(b, I, J) / units) * (K * b.per_k + b.rest);
+}
+
+// ... of both gradients': of workgroups of two kinds
+float pair_us(const Block& b, int64_t N, int D, int M, float units) {
+    const float x = M * b.per_k + b.rest, w = N * b.per_k + b.rest;
+    return 3.f + std::max(std::max(x, w), (blocks_of(b, N, D) * x + blocks_of(b, D, M) * w) / units + 0.5f * std::min(x, w));
+}
+
+template <class Us>
+int best_block(Us&& us) {
     int best = 0;
     for (int i = 1; i < (int)(sizeof(kBlocks) / sizeof(kBlocks[0])); ++i)
-        if (block_us(kBlocks[i], I, J, K, units) < block_us(kBlocks[best], I, J, K, units)) best = i;
+        if (us(kBlocks[i]) < us(kBlocks[best])) best = i;
     return best;
+}
+int best_block(int64_t I, int J, int64_t K) {
+    const float units = (float)compute_units();
+    return best_block([&](const Block& b) { return block_us(b, I, J, K, units); });
+}
+int best_pair(int64_t N, int D, int M) {
+    const float units = (float)compute_units();
+    return best_block([&](const Block& b) { return pair_us(b, N, D, M, units); });
+}
+
+// Calls f with the fragments of a block.
+template <class F>
+hipError_t with_block(int block, F&& f) {
+    using std::integral_constant;
+    switch (block) {
+        case 0: return f(integral_constant<int, 1>(), integral_constant<int, 1>());
+        case 1: return f(integral_constant<int, 2>(), integral_constant<int, 2>());
+        default: return f(integral_constant<int, 4>(), integral_constant<int, 2>());
+    }
+}
+
+// Sets the blocks; how many workgroups they take, 0 for too many.
+template <int FI, int FJ>
+int count_blocks(PlainArgs& a) {
+    const int64_t rows = (a.I + 16 * FI - 1) / (16 * FI), cols = (a.J + 16 * FJ - 1) / (16 * FJ);
+    if (rows * cols > (1 << 29)) return 0;
+    a.row_blocks = (int)rows, a.col_blocks = (int)cols;
+    return (int)(rows * cols + 7) / 8 * 8;
 }
 
 }  // namespace
@@ -228,27 +297,36 @@ hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, con
 }
 
 hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_t I, int J, int64_t K, const Epilogue& e, hipStream_t s) {
-    const auto with = [&](auto fi, auto fj) {
+    return with_block(best_block(I, J, K), [&](auto fi, auto fj) {
         constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
-        const int64_t row_blocks = (I + 16 * FI - 1) / (16 * FI), col_blocks = (J + 16 * FJ - 1) / (16 * FJ);
-        if (row_blocks * col_blocks > (1 << 30)) return hipErrorInvalidValue;
-        const auto launch = [&](auto ak, auto bk) {
-            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, decltype(ak)::value, decltype(bk)::value>),
-                               dim3((unsigned)(row_blocks * col_blocks + 7) / 8 * 8), dim3(kThreads), 0, s, A, B, I, J, K, (int)row_blocks,
-                               (int)col_blocks, e);
-            return hipGetLastError();
-        };
-        if (A.inner != 1) return launch(std::false_type(), std::false_type());
-        return B.inner == 1 ? launch(std::true_type(), std::true_type()) : launch(std::true_type(), std::false_type());
-    };
-    using std::integral_constant;
-    switch (best_block(I, J, K)) {
-        case 0: return with(integral_constant<int, 1>(), integral_constant<int, 1>());
-        case 1: return with(integral_constant<int, 2>(), integral_constant<int, 2>());
-        default: return with(integral_constant<int, 4>(), integral_constant<int, 2>());
-    }
+        PlainArgs a = {A, B, I, K, J, 0, 0, e};
+        const int blocks = count_blocks<FI, FJ>(a);
+        if (blocks == 0) return hipErrorInvalidValue;
+        if (A.inner != 1)
+            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, false, false>), dim3(blocks), dim3(kThreads), 0, s, a);
+        else if (B.inner == 1)
+            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, true, true>), dim3(blocks), dim3(kThreads), 0, s, a);
+        else
+            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, true, false>), dim3(blocks), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    });
 }
 
-float plain_f32_us(int64_t I, int J, int64_t K) { return block_us(kBlocks[best_block(I, J, K)], I, J, K, compute_units()); }
+float plain_f32_us(int64_t I, int J, int64_t K) { return block_us(kBlocks[best_block(I, J, K)], I, J, K, (float)compute_units()); }
+
+hipError_t launch_plain_pair_f32(const float* dZ, int64_t ldg, const float* W, int64_t ldw, const float* X, int64_t ldx, int64_t N, int D,
+                                 int M, const Epilogue& to_x, const Epilogue& to_w, const PartialSums& sums, hipStream_t s) {
+    return with_block(best_pair(N, D, M), [&](auto fi, auto fj) {
+        constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
+        PlainArgs x = {{dZ, ldg, 1}, {W, ldw, 1}, N, M, D, 0, 0, to_x}, w = {{X, 1, ldx}, {dZ, 1, ldg}, D, N, M, 0, 0, to_w};
+        const int x_blocks = count_blocks<FI, FJ>(x), w_blocks = count_blocks<FI, FJ>(w);
+        if (x_blocks == 0 || w_blocks == 0) return hipErrorInvalidValue;
+        const unsigned blocks = x_blocks + w_blocks + (sums.out ? (sums.width + 31) / 32 : 0);
+        hipLaunchKernelGGL((plain_pair_kernel<FI, FJ>), dim3(blocks), dim3(kThreads), 0, s, x, w, x_blocks, w_blocks, sums);
+        return hipGetLastError();
+    });
+}
+
+float plain_pair_us(int64_t N, int D, int M) { return pair_us(kBlocks[best_pair(N, D, M)], N, D, M, (float)compute_units()); }
 
 }  // namespace lutnn
