@@ -492,7 +492,7 @@ typedef enum {
  *
  *   X [N][D], W [D][M] (as lutnn_build_table), bias [M] fp32 or NULL, residual [N][M] or NULL
  *   Y [N][M]; preactivation [N][M] or NULL: receives Z, which the backward pass of an activation needs
- * D and M up to 2^24 - 512.  Errors: E_NULL, E_SHAPE, E_UNSUPPORTED (dtype, activation), E_ALIGN, E_HIP.
+ * D and M up to 2^21.  Errors: E_NULL, E_SHAPE, E_UNSUPPORTED (dtype, activation), E_ALIGN, E_HIP.
  */
 LUTNN_API lutnn_status lutnn_dense_linear(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw,
                                           int32_t D, int32_t M, const float* bias, int32_t activation, const void* residual,

@@ -1051,7 +1051,7 @@ lutnn_status lutnn_conv2d(const lutnn_layer* layer, const float* input, int64_t 
 // ---- the layers around the looked-up ones
 namespace {
 
-constexpr int kMaxWidth = (1 << 24) - 512;  // as check_dims
+constexpr int kMaxWidth = 1 << 21;  // a tile's rows of a laid-out matrix within 32-bit offsets
 
 int value_bytes(int32_t dtype) { return dtype == LUTNN_F32 ? 4 : 2; }
 

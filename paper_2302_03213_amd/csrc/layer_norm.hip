@@ -7,7 +7,7 @@
 // What bounds both: every matrix read or written once, at the rate of the memory.  A row lies in the registers of the threads
 // that share it, 16 values each, so that nothing is read twice: the sum of squares is that of the differences from the mean (two
 // reductions of a row, no cancellation).  Rows of up to 256 values take 16 threads, up to 1024 a wavefront, up to 4096 four, up
-// to 16384 sixteen.  Sums are fp32 ones.
+// to 8192 eight, up to 16384 sixteen.  Sums are fp32 ones.
 #include <algorithm>
 
 #include "lutnn_kernels.h"
@@ -143,7 +143,7 @@ struct NormGradientArgs {
 
 // Rows are dealt to the workgroups in turn; each keeps the column sums of its own in registers and leaves them in `partial`.  The fewer
 // workgroups, the fewer sums are left, so that the next row's loads have to hide the memory's latency: 16384 x 4096 in bf16 with a
-// residual 103 us, 537 MB at the rate of a large copy; 168 without them.
+// residual 107 us, 537 MB at the rate of a large copy; 168 without them.
 template <class T, int VEC, int TPR>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gradient_kernel(NormGradientArgs<T> a) {
     constexpr int THREADS = TPR < kThreads ? kThreads : TPR, ROWS = THREADS / TPR, CH = VEC == 1 ? 1 : kValues / VEC;
@@ -152,16 +152,20 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
     int turn = 0;
     const Columns<VEC, TPR> col{a.D, (int)(threadIdx.x % TPR)};
     float dw[CH][VEC] = {}, db[CH][VEC] = {}, w[CH][VEC];
+    const auto load_weight = [&] {
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-        if (col.any(c)) {
-            if (a.w)
-                load_values(a.w + col.at(c), w[c]);
-            else
+        for (int c = 0; c < CH; ++c)
+            if (col.any(c)) {
+                if (a.w)
+                    load_values(a.w + col.at(c), w[c]);
+                else
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) w[c][j] = 1.f;
-        }
-    // a row as it lies in memory; the next one is on its way while one is worked on
+                    for (int j = 0; j < VEC; ++j) w[c][j] = 1.f;
+            }
+    };
+    // a row as it lies in memory; the next one is on its way while one is worked on, where there are registers for it: sixteen
+    // wavefronts have 128 each
+    constexpr bool AHEAD = TPR < 1024;
     struct Row {
         typename Packed<T, VEC>::type g[CH], x[CH], r[CH];
         float mean, rstd;
@@ -186,10 +190,17 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
     };
     const int64_t first = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR, step = (int64_t)gridDim.x * ROWS;
     Row next;
-    fetch(next, first);
+    if constexpr (AHEAD) {
+        load_weight();
+        fetch(next, first);
+    }
     for (int64_t n = first; n < a.N; n += step) {
+        if constexpr (!AHEAD) fetch(next, n);
         const Row row = next;
-        fetch(next, n + step);
+        if constexpr (AHEAD)
+            fetch(next, n + step);
+        else
+            load_weight();
         float g[CH][VEC], h[CH][VEC], sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -265,15 +276,16 @@ hipError_t by_width(int D, F&& f) {
     if (D <= 16 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 16>());
     if (D <= 64 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 64>());
     if (D <= 256 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 256>());
+    if (D <= 512 * kValues) return f(integral_constant<int, V>(), integral_constant<int, 512>());
     return f(integral_constant<int, V>(), integral_constant<int, 1024>());
 }
 
 int rows_per_workgroup(int D) { return D <= 16 * kValues ? kThreads / 16 : D <= 64 * kValues ? kThreads / 64 : 1; }
 
-// Two workgroups per compute unit for rows within a wavefront, one for longer ones: 4096 x 768 in fp32 9.3 us (one: 9.6, four: 11.0),
-// 16384 x 4096 in bf16 with a residual 103 (two: 107, four: 115, eight: 125).
+// Two workgroups per compute unit, one for rows of more than four wavefronts.  4096 x 768 in fp32: 9.2 us (one: 9.6, four: 11.0); 16384 x 4096 in
+// bf16 82 (one: 101, three: 90), with a residual 107 (one: 104, three: 112).
 int gradient_workgroups(int64_t N, int D) {
-    const int64_t most = (D <= 64 * kValues ? 2 : 1) * (int64_t)compute_units();
+    const int64_t most = (D <= 256 * kValues ? 2 : 1) * (int64_t)compute_units();
     const int rows = rows_per_workgroup(D);
     return (int)std::min<int64_t>((N + rows - 1) / rows, most);
 }

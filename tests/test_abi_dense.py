@@ -79,7 +79,7 @@ def test_dense_linear_refusals(lut):
         assert call.refused(**{name: None}) == "LUTNN_E_NULL", name
     for act in (-1, 5):
         assert call.refused(act=act) == "LUTNN_E_UNSUPPORTED"
-    assert call.refused(M=0) == "LUTNN_E_SHAPE" and call.refused(M=1 << 24) == "LUTNN_E_SHAPE"
+    assert call.refused(M=0) == "LUTNN_E_SHAPE" and call.refused(M=(1 << 21) + 1, ldw=1 << 22, ldr=1 << 22, ldy=1 << 22, ldz=1 << 22) == "LUTNN_E_SHAPE"
     assert call.refused(N=0, X=None, W=None, Y=None, workspace=None) == "LUTNN_OK"
 
 
@@ -147,3 +147,13 @@ def test_python_refusals(lut):
         else:
             with pytest.raises(ValueError):
                 binding._vector("v", v, 8, like)
+
+
+def test_native_calls_leave_alone_what_is_not_plain(lut):
+    from paper_2302_03213_amd import binding
+    calls, X, v = binding._calls, torch.zeros(4, 8), torch.zeros(8)
+    assert calls.dense_linear(X, X, None, 0, None, None) is None
+    assert calls.dense_linear(X, X, None, 0) is None
+    assert calls.dense_linear_backward(X, X, X, None, 0, True, True, True) is None
+    assert calls.layer_norm(X, v, v, 1e-5, None, None, None) is None
+    assert calls.layer_norm_backward(X, X, X, None, None, True, True, True) is None

@@ -65,6 +65,32 @@ def test_backward(lut, N, D, M, kind):
             du.check(g, want, off)
 
 
+# sizes that fill the chip with the large tiles, leave a few tiles over, and have long sums with few outputs
+LARGE = [(4096, 768, 2304), (2000, 640, 640), (513, 2048, 1032), (64, 4096, 512), (8192, 264, 4096), (1000, 4104, 264), (8200, 2056, 2040),
+         (4099, 1000, 1800)]
+
+
+@pytest.mark.parametrize("kind", list(du.TYPES))
+@pytest.mark.parametrize("N,D,M", LARGE)
+def test_large(lut, N, D, M, kind):
+    T = du.TYPES[kind]
+    X, W, b, R, G = operands(N, D, M, T, seed=N + D + M)
+    for activation, residual, keep in (("gelu", None, True), (None, R, False), ("silu", R, False)):
+        Z = torch.full_like(R, float("nan")) if keep else None
+        Y = lut.dense_linear(X, W, b, activation, residual, preactivation=Z)
+        y, y_off, z, z_off = du.dense64(X, W, b, activation, residual)
+        du.check(Y, y, y_off)
+        if keep:
+            du.check(Z, z, z_off)
+    for activation in (None, "gelu_tanh"):
+        wanted = du.dense_backward64(X, W, G, R, activation)
+        for needs in ((True, True, True), (True, False, False), (False, True, True)):
+            got = lut.dense_linear_backward(X, W, G, R if activation else None, activation, *needs)
+            for g, (want, off) in zip(got, wanted):
+                if g is not None:
+                    du.check(g, want, off)
+
+
 @pytest.mark.parametrize("needs", list(itertools.product((False, True), repeat=3)))
 def test_what_is_not_needed_changes_nothing(lut, needs):
     X, W, _, _, G = operands(70, 136, 72, torch.bfloat16, seed=3)
@@ -114,8 +140,8 @@ def test_no_rows(lut, kind):
 def test_values_that_are_not_finite_stay_where_they_belong(lut, kind):
     """An infinite or missing value reaches its row (of X) or its column (of W) alone, as what the sums make of it."""
     T = du.TYPES[kind]
-    for N in (6, 150):
-        X, W, b, R, G = operands(N, 136, 72, T, seed=21)
+    for N, M in ((6, 72), (150, 72), (2500, 640)):
+        X, W, b, R, G = operands(N, 136, M, T, seed=21)
         X[2, 7], X[4, 130] = float("inf"), float("nan")
         W[5, 11] = float("-inf")
         with_inf = X.float() @ W.float() + b
@@ -132,10 +158,13 @@ def test_values_that_are_not_finite_stay_where_they_belong(lut, kind):
 def test_fp32_values_of_any_size(lut):
     """Very large and very small operands keep the precision of fp32 products."""
     for exponent in (-50, -30, 30, 50):
-        X, W, _, _, _ = operands(140, 200, 136, torch.float32, seed=8)
-        X, W = X * 2.0 ** exponent, W * 2.0 ** (exponent // 2)
-        y, y_off, _, _ = du.dense64(X, W)
-        du.check(lut.dense_linear(X, W), y, y_off)
+        for N in (3, 140, 2100):
+            X, W, _, _, G = operands(N, 200, 520, torch.float32, seed=8)
+            X, W = X * 2.0 ** exponent, W * 2.0 ** (exponent // 2)
+            y, y_off, _, _ = du.dense64(X, W)
+            du.check(lut.dense_linear(X, W), y, y_off)
+            for g, (want, off) in zip(lut.dense_linear_backward(X, W, G), du.dense_backward64(X, W, G, None, None)):
+                du.check(g, want, off)
 
 
 @pytest.mark.parametrize("kind", list(du.TYPES))
@@ -252,3 +281,54 @@ def test_module_refuses_capture(lut):
     torch.cuda.synchronize()
     eager.backward(G)
     assert torch.isfinite(layer.W.grad).all()
+
+
+@pytest.mark.parametrize("kind", list(du.TYPES))
+def test_the_python_way_agrees(lut, kind, monkeypatch):
+    from paper_2302_03213_amd import binding
+    X, W, b, R, G = operands(70, 40, 24, du.TYPES[kind], seed=17)
+    Z = torch.empty_like(R)
+
+    def results():
+        return (lut.dense_linear(X, W, b, "gelu", R, preactivation=Z), *lut.dense_linear_backward(X, W, G, R, "silu"),
+                lut.dense_linear_backward(X, W, G, None, None, False, True, False)[1])
+
+    native = results()
+    monkeypatch.setattr(binding, "_calls", binding._NoCalls())
+    for a, c in zip(native, results()):
+        assert torch.equal(a, c)
+
+
+def test_tensors_that_are_refused(lut):
+    X, W, b, R, G = operands(6, 8, 16, torch.bfloat16, seed=18)
+    for call in (lambda: lut.dense_linear(X, W.t()), lambda: lut.dense_linear(X, W.float()), lambda: lut.dense_linear(X, W, b[:8]),
+                 lambda: lut.dense_linear(X, W, b.to(X.dtype)), lambda: lut.dense_linear(X, W, b, "swish"),
+                 lambda: lut.dense_linear(X, W, residual=R[:3]), lambda: lut.dense_linear(X, W.t().contiguous().t()),
+                 lambda: lut.dense_linear(X.double(), W.double()), lambda: lut.dense_linear(X, W.cpu()),
+                 lambda: lut.dense_linear(X, W, out=R[:3]), lambda: lut.dense_linear_backward(X, W, G, None, "gelu"),
+                 lambda: lut.dense_linear_backward(X[:5], W, G), lambda: lut.dense_linear_backward(X, W, G, G[:2], "relu")):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(lut.LutnnError) as e:  # rows on top of each other
+        lut.dense_linear(X[:1].expand(6, 8), W)
+    assert e.value.name == "LUTNN_E_SHAPE"
+
+
+def test_two_graphs_of_one_pool(lut):
+    """Workspaces of two graphs may be the same memory: replayed one after the other, each gives its own result."""
+    sets = [operands(N, 264, 520, torch.float32, seed=N) for N in (2200, 1500)]
+    for X, W, b, R, G in sets:
+        lut.dense_linear(X, W, b)
+    graphs, outs, pool = [], [], None
+    for X, W, b, R, G in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=pool):
+            outs.append((lut.dense_linear(X, W, b, "gelu"), *lut.dense_linear_backward(X, W, G)))
+        graphs.append(graph)
+        pool = graph.pool()
+    wanted = [(lut.dense_linear(X, W, b, "gelu"), *lut.dense_linear_backward(X, W, G)) for X, W, b, R, G in sets]
+    for i in (0, 1, 1, 0, 1):
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        for a, c in zip(outs[i], wanted[i]):
+            assert torch.equal(a, c)

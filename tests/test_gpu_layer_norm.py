@@ -33,8 +33,8 @@ def operands(N, D, T, seed, shift=0.0):
 
 # widths around vectors, wavefronts and the steps of the threads per row
 SIZES = [(1, 1), (3, 2), (5, 3), (4, 7), (9, 8), (17, 9), (33, 63), (2, 64), (40, 65), (16, 255), (31, 256), (33, 257), (1, 768),
-         (130, 768), (7, 1000), (5, 1023), (6, 1024), (6, 1025), (3, 2049), (600, 1536), (2, 4095), (3, 4096), (3, 4097), (2, 9000),
-         (2, 16383), (3, 16384), (5000, 40), (2100, 264)]
+         (130, 768), (7, 1000), (5, 1023), (6, 1024), (6, 1025), (3, 2049), (600, 1536), (2, 4095), (3, 4096), (3, 4097), (2, 9000), (3, 8192), (4, 5120),
+                  (2, 16383), (3, 16384), (5000, 40), (2100, 264)]
 
 
 @pytest.mark.parametrize("kind", list(du.TYPES))
@@ -240,3 +240,34 @@ def test_module_without_residual_and_refusals(lut):
             norm(X).backward(G)
     torch.cuda.synchronize()
     eager.backward(G)
+
+
+@pytest.mark.parametrize("kind", list(du.TYPES))
+def test_the_python_way_agrees(lut, kind, monkeypatch):
+    from paper_2302_03213_amd import binding
+    X, R, G, w, b = operands(70, 40, du.TYPES[kind], seed=17)
+    statistics, total = torch.empty((70, 2), device="cuda"), torch.empty_like(X)
+
+    def results():
+        return (lut.layer_norm(X, w, b, EPS, R, total=total, statistics=statistics), total.clone(), statistics.clone(),
+                *lut.layer_norm_backward(G, total, statistics, w, R))
+
+    native = results()
+    monkeypatch.setattr(binding, "_calls", binding._NoCalls())
+    for a, c in zip(native, results()):
+        assert torch.equal(a, c)
+
+
+def test_tensors_that_are_refused(lut):
+    X, R, G, w, b = operands(6, 8, torch.bfloat16, seed=18)
+    statistics = torch.empty((6, 2), device="cuda")
+    for call in (lambda: lut.layer_norm(X, w[:4]), lambda: lut.layer_norm(X, w.to(X.dtype)), lambda: lut.layer_norm(X, w, b, residual=R[:3]),
+                 lambda: lut.layer_norm(X.t()), lambda: lut.layer_norm(X.double()), lambda: lut.layer_norm(X, statistics=statistics[:3]),
+                 lambda: lut.layer_norm(X, residual=R.float()), lambda: lut.layer_norm_backward(G, X, statistics.t()),
+                 lambda: lut.layer_norm_backward(G, X.float(), statistics), lambda: lut.layer_norm_backward(G, X, statistics, w.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: lut.layer_norm(X, total=R), lambda: lut.layer_norm(X, eps=-1.0), lambda: lut.layer_norm(X[:1].expand(6, 8)),
+                 lambda: lut.layer_norm(torch.zeros(2, 16392, device="cuda"))):
+        with pytest.raises(lut.LutnnError):
+            call()
