@@ -492,7 +492,7 @@ typedef enum {
  *
  *   X [N][D], W [D][M] (as lutnn_build_table), bias [M] fp32 or NULL, residual [N][M] or NULL
  *   Y [N][M]; preactivation [N][M] or NULL: receives Z, which the backward pass of an activation needs
- * D and M up to 2^21.  Errors: E_NULL, E_SHAPE, E_UNSUPPORTED (dtype, activation), E_ALIGN, E_HIP.
+ * D and M up to 2^21, ceil(N / 128) * ceil(max(D, M) / 256) too.  Errors: E_NULL, E_SHAPE, E_UNSUPPORTED (dtype, activation), E_ALIGN, E_HIP.
  */
 LUTNN_API lutnn_status lutnn_dense_linear(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw,
                                           int32_t D, int32_t M, const float* bias, int32_t activation, const void* residual,
@@ -529,6 +529,7 @@ LUTNN_API size_t lutnn_dense_linear_backward_workspace_bytes(int32_t dtype, cons
  *
  *   X [N][D], residual [N][D] or NULL, weight and bias [D] fp32 or NULL (ones, zeros), eps >= 0
  *   Y [N][D]; total [N][D] or NULL: receives S (with a residual only); statistics [N][2] fp32 or NULL: receives mean and rstd
+ *   Y and the statistics are those of S before it is rounded to `dtype`.
  *   D up to 16384 (E_UNSUPPORTED above)
  * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
  */

@@ -2,6 +2,7 @@
 // include/lutnn.h.  Nothing here allocates device memory or synchronises.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -1052,6 +1053,7 @@ lutnn_status lutnn_conv2d(const lutnn_layer* layer, const float* input, int64_t 
 namespace {
 
 constexpr int kMaxWidth = 1 << 21;  // a tile's rows of a laid-out matrix within 32-bit offsets
+constexpr int64_t kMaxTiles = 1 << 21;  // of 128 x 256: a launch has 2^32 threads at most
 
 int value_bytes(int32_t dtype) { return dtype == LUTNN_F32 ? 4 : 2; }
 
@@ -1086,7 +1088,10 @@ lutnn_status check_dense(int32_t dtype, int64_t N, int32_t D, int32_t M, int32_t
     if (activation < LUTNN_ACTIVATION_NONE || activation > LUTNN_ACTIVATION_SILU)
         return fail(LUTNN_E_UNSUPPORTED, "unknown activation %d", activation);
     if (D <= 0 || M <= 0 || D > kMaxWidth || M > kMaxWidth) return fail(LUTNN_E_SHAPE, "D=%d or M=%d out of range", D, M);
-    return check_rows(N);
+    if (lutnn_status st = check_rows(N)) return st;
+    if ((N + 127) / 128 * ((std::max(D, M) + 255) / 256) > kMaxTiles)
+        return fail(LUTNN_E_SHAPE, "N=%lld rows of %d values: more than a launch can share out", (long long)N, std::max(D, M));
+    return LUTNN_OK;
 }
 
 lutnn_status check_workspace(const void* workspace, size_t given, size_t needed) {

@@ -212,7 +212,7 @@ float tiles_us(const TileSize& t, float count, float stages, float units) {
 
 // The fastest by those figures.  A sum is shared out where the last tiles would leave most of the chip idle for longer than a second
 // launch, which adds up what the first left in memory, takes.  k_rows: how many of the two operands run along k; laid-out fp32 ones
-// are read in pieces of 64 bytes then, which takes small tiles a sixth longer.
+// are read in pieces of 64 bytes then, which takes tiles 5 to 20 % longer (by_rows).
 Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 5, units = compute_units();
@@ -220,15 +220,16 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows) {
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
+        if (tiles > kMostTiles) continue;
         const float stage = t.depth / 64.f * (dtype == 0 && k_rows == 2 ? t.by_rows : 1.f);
         const float us = kLaunchUs + tiles_us(t, (float)tiles, k_tiles * stage, (float)units);
-        if (us < best.us) best = {i, (int)std::min<int64_t>(tiles, 1 << 29), 1, tiles, us};
+        if (us < best.us) best = {i, (int)tiles, 1, tiles, us};
         const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
         const float base = kLaunchUs + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
         if (shared == 0) continue;
         for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / kBytesPerUs;
-            if (splits > k_tiles || moved >= best.us) break;
+            if (splits > k_tiles || moved >= best.us || shared * splits > kMostTiles) break;
             const float shared_us = moved + tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units);
             if (shared_us < best.us) best = {i, (int)whole, splits, tiles, shared_us};
         }
@@ -251,6 +252,7 @@ PairPlan pair_plan(int dtype, int64_t N, int D, int M) {
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t x_tiles = ((N + t.i - 1) / t.i) * ((D + t.j - 1) / t.j), w_tiles = ((int64_t)(D + t.i - 1) / t.i) * ((M + t.j - 1) / t.j);
+        if (std::max(x_tiles, w_tiles) > kMostTiles) continue;
         const float x_stages = (float)((M + t.depth - 1) / t.depth), w_stages = (float)((N + t.depth - 1) / t.depth);
         const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / kBytesPerUs;
         for (const int xs : {1, 2, 4}) {
@@ -259,7 +261,7 @@ PairPlan pair_plan(int dtype, int64_t N, int D, int M) {
                 if (ws > 1 && (ws > w_stages || w_tiles * ws > 4 * slots)) break;
                 const float nx = (float)x_tiles * xs, nw = (float)w_tiles * ws;
                 const float kx = std::ceil(x_stages / xs) * unit * t.by_rows, kw = std::ceil(w_stages / ws) * unit;
-                // alone as many at once as there are; else the work by the slots, and half the longer tile for the end
+                // alone as many at once as there are; else the work by the slots, and two fifths of the longer tile for the end
                 const int at_once = std::min((int)std::ceil((nx + nw) / units), t.at_once) - 1;
                 const float x = kx * t.stage[at_once] + t.rest[at_once], w = kw * t.stage[at_once] + t.rest[at_once];
                 float us = std::max(x, w);
@@ -383,10 +385,6 @@ size_t slope_bytes(const DenseCall& c, const GradientPlan& g) {
     return g.plain ? (size_t)round_up(c.N * c.M * 4, 256) : laid_out_bytes(c.dtype, c.N, c.M);
 }
 size_t column_bytes(const GradientPlan& g, int M) { return g.sums ? (size_t)round_up((int64_t)g.slope.chunks * M * 4, 256) : 0; }
-
-}  // namespace
-
-namespace {
 
 // How a forward pass goes: few rows, plain fp32, or tiles of operands that may have to be laid out.
 struct ForwardPlan {

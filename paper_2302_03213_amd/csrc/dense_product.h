@@ -65,6 +65,13 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// What a wavefront's lanes have written to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // 64 lanes x 16 bytes from the buffer `rsrc` straight into LDS at lds_dst + 16 * lane; zeros for offsets past its end.  Nothing
 // is said of LDS being written: reads of other buffers may move across, and wait_loads keeps those of this one behind it.
 __device__ __forceinline__ void buffer_to_lds(uint32_t lds_dst, i32x4 rsrc, uint32_t voff) {
@@ -413,6 +420,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
 #pragma unroll
     for (int round = 0; round < ROUNDS; ++round) {
         float probe = 0.f;
+        if (round > 0) wave_sync();  // the last round has been read
 #pragma unroll
         for (int i = 0; i < ROUND / 16; ++i)
 #pragma unroll
@@ -424,6 +432,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
                 }
                 *reinterpret_cast<f32x4*>(out + (16 * i + lane % 16) * PITCH + 16 * j + 4 * (lane / 16)) = z;
             }
+        wave_sync();
         if constexpr (F32)
             // sums that are not finite are formed again: an infinite value has no parts
             if (splits == 1 && __any(!is_finite(probe))) {
@@ -434,6 +443,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
                     float& z = out[v / COLS * PITCH + v % COLS];
                     if (i < a.I && j < a.J && !is_finite(z)) z = chain(a, i, j);
                 }
+                wave_sync();
             }
         if (round + 1 < ROUNDS) fetch(round + 1);
         if (added) {
@@ -523,11 +533,11 @@ inline unsigned blocks_of(const ProductArgs& a) {
     return (a.whole + 7) / 8 * 8 + (shared * a.splits + 7) / 8 * 8;
 }
 
-// Sets i_tiles and j_tiles; false for more tiles than a grid has.
+// Sets i_tiles and j_tiles; false for too many.
 template <class C>
 bool count_tiles(ProductArgs& a) {
     const int64_t i_tiles = (a.I + C::TI - 1) / C::TI, j_tiles = (a.J + C::TJ - 1) / C::TJ, tiles = i_tiles * j_tiles;
-    if (tiles > (1 << 29) || (tiles - a.whole) * a.splits > (1 << 29)) return false;
+    if (tiles > kMostTiles || (tiles - a.whole) * a.splits > kMostTiles) return false;
     a.i_tiles = (int)i_tiles, a.j_tiles = (int)j_tiles;
     return true;
 }
@@ -544,7 +554,7 @@ hipError_t join(const ProductArgs& a, hipStream_t s) {
 // a.whole: how many tiles not to share.  A's k is inner but for dW = X^T dZ, B's for dX = dZ W^T.
 template <class C>
 hipError_t launch(ProductArgs a, bool a_k, bool b_k, hipStream_t s) {
-    if (!count_tiles<C>(a)) return hipErrorInvalidValue;
+    if (!count_tiles<C>(a)) return hipErrorInvalidConfiguration;
     const dim3 grid(blocks_of(a)), threads(C::THREADS);
     if (!a_k)
         hipLaunchKernelGGL((product_kernel<C, false, false>), grid, threads, 0, s, a);
@@ -558,7 +568,7 @@ hipError_t launch(ProductArgs a, bool a_k, bool b_k, hipStream_t s) {
 
 template <class C>
 hipError_t launch_pair(PairArgs p, hipStream_t s) {
-    if (!count_tiles<C>(p.x) || !count_tiles<C>(p.w)) return hipErrorInvalidValue;
+    if (!count_tiles<C>(p.x) || !count_tiles<C>(p.w)) return hipErrorInvalidConfiguration;
     p.x_blocks = (int)blocks_of(p.x), p.w_blocks = (int)blocks_of(p.w);
     const unsigned blocks = p.x_blocks + p.w_blocks + (p.sums.out ? (p.sums.width + 31) / 32 : 0);
     hipLaunchKernelGGL(pair_kernel<C>, dim3(blocks), dim3(C::THREADS), 0, s, p);

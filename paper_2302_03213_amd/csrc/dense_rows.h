@@ -4,6 +4,9 @@
 
 namespace lutnn {
 
+// Tiles of a product: a launch has 2^32 threads at most.
+constexpr int64_t kMostTiles = 1 << 21;
+
 // Up to this many rows go through the kernel for single tokens.
 constexpr int kFewRows = 4;
 

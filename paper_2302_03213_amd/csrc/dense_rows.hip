@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(const T* __restrict_
         float w[n][V], x[n][ROWS];
 #pragma unroll
         for (int a = 0; a < n; ++a) {
-            const int64_t k = min(k0 + a * STEP, D - 1);  // past the last row: that one, times zero
+            const int64_t k = min(k0 + a * STEP, D - 1);  // past the last row: that one, and not added
             const T* const from = W + k * ldw + j;
             if (whole)
                 load_values(from, w[a]);
@@ -234,11 +234,13 @@ float blocks_of(const Block& b, int64_t I, int J) {
 
 // A launch, and rounds of workgroups.
 float block_us(const Block& b, int64_t I, int J, int64_t K, float units) {
+    if (blocks_of(b, I, J) > kMostTiles) return 1e30f;
     return 3.f + std::ceil(blocks_of(b, I, J) / units) * (K * b.per_k + b.rest);
 }
 
 // ... of both gradients': of workgroups of two kinds
 float pair_us(const Block& b, int64_t N, int D, int M, float units) {
+    if (std::max(blocks_of(b, N, D), blocks_of(b, D, M)) > kMostTiles) return 1e30f;
     const float x = M * b.per_k + b.rest, w = N * b.per_k + b.rest;
     return 3.f + std::max(std::max(x, w), (blocks_of(b, N, D) * x + blocks_of(b, D, M) * w) / units + 0.5f * std::min(x, w));
 }
@@ -274,7 +276,7 @@ hipError_t with_block(int block, F&& f) {
 template <int FI, int FJ>
 int count_blocks(PlainArgs& a) {
     const int64_t rows = (a.I + 16 * FI - 1) / (16 * FI), cols = (a.J + 16 * FJ - 1) / (16 * FJ);
-    if (rows * cols > (1 << 29)) return 0;
+    if (rows * cols > kMostTiles) return 0;
     a.row_blocks = (int)rows, a.col_blocks = (int)cols;
     return (int)(rows * cols + 7) / 8 * 8;
 }
@@ -301,7 +303,7 @@ hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_
         constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
         PlainArgs a = {A, B, I, K, J, 0, 0, e};
         const int blocks = count_blocks<FI, FJ>(a);
-        if (blocks == 0) return hipErrorInvalidValue;
+        if (blocks == 0) return hipErrorInvalidConfiguration;
         if (A.inner != 1)
             hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, false, false>), dim3(blocks), dim3(kThreads), 0, s, a);
         else if (B.inner == 1)
@@ -320,7 +322,7 @@ hipError_t launch_plain_pair_f32(const float* dZ, int64_t ldg, const float* W, i
         constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
         PlainArgs x = {{dZ, ldg, 1}, {W, ldw, 1}, N, M, D, 0, 0, to_x}, w = {{X, 1, ldx}, {dZ, 1, ldg}, D, N, M, 0, 0, to_w};
         const int x_blocks = count_blocks<FI, FJ>(x), w_blocks = count_blocks<FI, FJ>(w);
-        if (x_blocks == 0 || w_blocks == 0) return hipErrorInvalidValue;
+        if (x_blocks == 0 || w_blocks == 0) return hipErrorInvalidConfiguration;
         const unsigned blocks = x_blocks + w_blocks + (sums.out ? (sums.width + 31) / 32 : 0);
         hipLaunchKernelGGL((plain_pair_kernel<FI, FJ>), dim3(blocks), dim3(kThreads), 0, s, x, w, x_blocks, w_blocks, sums);
         return hipGetLastError();

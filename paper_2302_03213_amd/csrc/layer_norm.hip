@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kValues = 16;     // of a row, per thread
 constexpr int kThreads = 256;   // per workgroup, but for rows that take more
+constexpr int kMostBlocks = 1 << 21;  // a launch may have 2^32 threads
 
 template <class T>
 constexpr int kVector = 16 / sizeof(T);  // values per load
@@ -69,65 +70,66 @@ struct NormArgs {
     float eps;
 };
 
-// grid: rows, kThreads / TPR (or one) of them per workgroup.
+// kThreads / TPR rows (or one) per workgroup, the first ones and then every grid's worth further.
 template <class T, int VEC, int TPR>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_kernel(NormArgs<T> a) {
     constexpr int ROWS = TPR < kThreads ? kThreads / TPR : 1, CH = VEC == 1 ? 1 : kValues / VEC;
     __shared__ float shared[2 * (TPR > 64 ? TPR / 64 : 1)];
     int turn = 0;
-    const int64_t n = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-    if (n >= a.N) return;  // whole wavefronts or, in groups of 16, nobody that the others wait for
     const Columns<VEC, TPR> col{a.D, (int)(threadIdx.x % TPR)};
-    float x[CH][VEC], total[1] = {0.f};
+    // rows that end earlier than a workgroup's others are whole wavefronts' or, in groups of 16, nobody that those wait for
+    for (int64_t n = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; n < a.N; n += (int64_t)gridDim.x * ROWS) {
+        float x[CH][VEC], total[1] = {0.f};
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        if (!col.any(c)) continue;
-        load_values(a.X + n * a.ldx + col.at(c), x[c]);
-        if (a.R) {
-            float r[VEC];
-            load_values(a.R + n * a.ldr + col.at(c), r);
+        for (int c = 0; c < CH; ++c) {
+            if (!col.any(c)) continue;
+            load_values(a.X + n * a.ldx + col.at(c), x[c]);
+            if (a.R) {
+                float r[VEC];
+                load_values(a.R + n * a.ldr + col.at(c), r);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) x[c][j] += r[j];
-            if (a.S) store_values(a.S + n * a.lds + col.at(c), x[c]);
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) total[0] += col.mine(c, j) ? x[c][j] : 0.f;
-    }
-    row_sums<TPR>(total, shared, turn);
-    const float mean = total[0] / a.D;
-    float squares[1] = {0.f};
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-        if (col.any(c))
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                x[c][j] -= mean;
-                squares[0] += col.mine(c, j) ? x[c][j] * x[c][j] : 0.f;
+                for (int j = 0; j < VEC; ++j) x[c][j] += r[j];
+                if (a.S) store_values(a.S + n * a.lds + col.at(c), x[c]);
             }
-    row_sums<TPR>(squares, shared, turn);
-    const float rstd = 1.f / sqrtf(squares[0] / a.D + a.eps);
-    if (a.statistics && col.t == 0) {
-        a.statistics[2 * n] = mean;
-        a.statistics[2 * n + 1] = rstd;
-    }
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        if (!col.any(c)) continue;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) x[c][j] *= rstd;
-        if (a.w) {
-            float w[VEC];
-            load_values(a.w + col.at(c), w);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) x[c][j] *= w[j];
+            for (int j = 0; j < VEC; ++j) total[0] += col.mine(c, j) ? x[c][j] : 0.f;
         }
-        if (a.b) {
-            float b[VEC];
-            load_values(a.b + col.at(c), b);
+        row_sums<TPR>(total, shared, turn);
+        const float mean = total[0] / a.D;
+        float squares[1] = {0.f};
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) x[c][j] += b[j];
+        for (int c = 0; c < CH; ++c)
+            if (col.any(c))
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    x[c][j] -= mean;
+                    squares[0] += col.mine(c, j) ? x[c][j] * x[c][j] : 0.f;
+                }
+        row_sums<TPR>(squares, shared, turn);
+        const float rstd = 1.f / sqrtf(squares[0] / a.D + a.eps);
+        if (a.statistics && col.t == 0) {
+            a.statistics[2 * n] = mean;
+            a.statistics[2 * n + 1] = rstd;
         }
-        store_values(a.Y + n * a.ldy + col.at(c), x[c]);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!col.any(c)) continue;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[c][j] *= rstd;
+            if (a.w) {
+                float w[VEC];
+                load_values(a.w + col.at(c), w);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) x[c][j] *= w[j];
+            }
+            if (a.b) {
+                float b[VEC];
+                load_values(a.b + col.at(c), b);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) x[c][j] += b[j];
+            }
+            store_values(a.Y + n * a.ldy + col.at(c), x[c]);
+        }
     }
 }
 
@@ -303,7 +305,7 @@ hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, i
                             statistics, N, ldx, ldr, ldy, lds, D, eps};
         return by_width<T>(D, [&](auto vec, auto tpr) {
             constexpr int TPR = decltype(tpr)::value, ROWS = TPR < kThreads ? kThreads / TPR : 1;
-            hipLaunchKernelGGL((layer_norm_kernel<T, decltype(vec)::value, TPR>), dim3((unsigned)((N + ROWS - 1) / ROWS)),
+            hipLaunchKernelGGL((layer_norm_kernel<T, decltype(vec)::value, TPR>), dim3((unsigned)std::min<int64_t>((N + ROWS - 1) / ROWS, kMostBlocks)),
                                dim3(TPR < kThreads ? kThreads : TPR), 0, s, a);
             return hipGetLastError();
         });

@@ -81,6 +81,8 @@ def test_dense_linear_refusals(lut):
         assert call.refused(act=act) == "LUTNN_E_UNSUPPORTED"
     assert call.refused(M=0) == "LUTNN_E_SHAPE" and call.refused(M=(1 << 21) + 1, ldw=1 << 22, ldr=1 << 22, ldy=1 << 22, ldz=1 << 22) == "LUTNN_E_SHAPE"
     assert call.refused(N=0, X=None, W=None, Y=None, workspace=None) == "LUTNN_OK"
+    assert call.refused(N=(1 << 28) + 1) == "LUTNN_E_SHAPE"  # 2^21 tiles of 128 rows
+    assert call.refused(N=(1 << 27) + 1, M=257, ldw=264, ldr=264, ldy=264, ldz=264) == "LUTNN_E_SHAPE"
 
 
 def test_dense_linear_backward_refusals(lut):

@@ -228,6 +228,25 @@ def test_long_rows_and_many_outputs(lut):
     du.check(lut.dense_linear(far, W), y, off)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_many_narrow_rows(lut, kind):
+    """More blocks of 16 rows than a launch has workgroups.  dW and dbias are whole numbers that fp32 holds in any order."""
+    N, T = (1 << 25) + 77, du.TYPES[kind]
+    X = torch.zeros((N, 3), dtype=T, device="cuda")
+    X[::16] = 1
+    X[-1] = 1
+    W = torch.tensor([[1, 2], [3, 4], [5, 6]], dtype=T, device="cuda")
+    Y = lut.dense_linear(X, W, torch.ones(2, device="cuda"))
+    assert torch.equal(Y, X[:, :1] * torch.tensor([9, 12], dtype=T, device="cuda") + 1)
+    G = torch.ones((N, 2), dtype=T, device="cuda")
+    G[1::2] = 0
+    G[-2:] = 1
+    dX, dW, db = lut.dense_linear_backward(X, W, G)
+    assert torch.equal(dX, G[:, :1] * torch.tensor([3, 7, 11], dtype=T, device="cuda"))
+    count = torch.tensor(int((X[:, 0] * G[:, 0]).double().sum()), device="cuda")
+    assert torch.equal(dW, count.to(T).expand(3, 2)) and db.eq(float(G[:, 0].double().sum())).all()
+
+
 @pytest.mark.parametrize("kind", list(du.TYPES))
 def test_module_gradients(lut, kind):
     """The module's gradients are the call's; fp32 ones are also those of differences."""

@@ -148,6 +148,26 @@ def test_offsets_past_32_bits(lut):
         du.check(Y[at:at + 16], *y)
 
 
+@pytest.mark.parametrize("D", [1, 5])
+def test_more_rows_than_a_launch_has_workgroups_for(lut, D):
+    N = (1 << 25) + 33  # 2^21 workgroups of 16 rows, and some
+    X = torch.zeros((N, D), dtype=torch.bfloat16, device="cuda")
+    small = du.random((40, D), torch.bfloat16, D)
+    X[:40] = small
+    X[-40:] = small
+    statistics = torch.full((N, 2), float("nan"), device="cuda")
+    Y = lut.layer_norm(X, eps=EPS, statistics=statistics)
+    y, _, _, _ = du.norm64(small, None, None, EPS, None)
+    du.check(Y[:40], *y)
+    du.check(Y[-40:], *y)
+    assert not Y[40:-40].any() and torch.isfinite(statistics).all()
+    G = torch.ones_like(X)
+    G[:-8] = 0
+    dX, dw, db = lut.layer_norm_backward(G, X, statistics)
+    assert db.eq(8).all() and not dX[:-8].any()
+    torch.testing.assert_close(dw.double(), Y[-8:].double().sum(0), rtol=0, atol=8 * 4 * 2.0 ** -8)  # of values below 4 in bf16
+
+
 @pytest.mark.parametrize("kind", list(du.TYPES))
 def test_other_streams_and_repeats(lut, kind):
     X, R, G, w, b = operands(3000, 768, du.TYPES[kind], seed=4)
