@@ -5,7 +5,8 @@
 // The three products run on the matrix cores (dense_product.h), which want 16-bit operands whose rows are whole aligned 16-byte
 // vectors.  Matrices that are such go to them as they are; others are laid out in the workspace first: fp32 ones as three planes of
 // bf16 parts, 16-bit ones of odd widths, strides or addresses as copies with padded rows.  dZ is formed on the way there, and summed
-// for db in the same pass.
+// for db in the same pass: 8192 x 4096 in bf16 with the slope of gelu_tanh 44 us, 4.6 TB/s.  fp32 products too small for that go
+// through the fp32 instructions as they are (dense_tile_f32.h, dense_rows.hip), and so do a few rows of any type (dense_rows.hip).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -175,29 +176,36 @@ hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db
     });
 }
 
-// The tiles of launch_tile (dense_product.h), how many of them a compute unit holds, and what 1 .. that many at once take, in us: per
-// 64 k, and beside that.  From products of 16 x 16 n tiles at K = 512 and 2560, the three layouts' average.  Small tiles are bound by
-// what a compute unit gets from L2 (75 GB/s), the large ones by the matrix instructions and the power they draw.
+// The tiles of with_tile (dense_product.h), how many of them a compute unit holds, and what 1 .. that many at once take, in us: per
+// 64 k, and beside that.  16 bits: from products of 16 x 16 n tiles at K = 512 and 2560, the three layouts' average.  Small tiles are
+// bound by what a compute unit gets from L2 (75 GB/s), the large ones by the matrix instructions and the power they draw.  fp32: fitted
+// to the times of 28 sizes from 8 x 768 x 768 to 4096 x 4096 x 768, three products each, which they then order so that the choice
+// takes 1.2 % longer than the best of all; tiles of 64 x 64 and 64 x 128 from planes were the best of none by more than 1 %.
 struct TileSize {
     int i, j, depth, at_once;
-    float stage[4], rest[4], by_rows = 1.f;
+    float stage[4], rest[4];
+    bool as_is = false;  // of fp32 operands that are not laid out
 };
 constexpr TileSize kTiles16[] = {{256, 256, 32, 1, {1.55f}, {9.0f}},
                                  {128, 128, 64, 2, {0.78f, 0.90f}, {2.0f, 5.0f}},
                                  {64, 128, 64, 2, {0.61f, 0.65f}, {0.5f, 2.5f}},
                                  {64, 64, 64, 3, {0.23f, 0.46f, 0.66f}, {1.0f, 0.7f, 1.0f}},
                                  {32, 64, 64, 4, {0.16f, 0.37f, 0.56f, 0.72f}, {1.0f, 0.5f, 0.5f, 0.5f}}};
-constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {4.1f}, {12.0f}, 1.05f},
-                                  {128, 128, 32, 1, {2.35f}, {4.5f}, 1.10f},
-                                  {64, 128, 32, 2, {1.9f, 2.5f}, {0.5f, 5.5f}, 1.16f},
-                                  {64, 64, 32, 3, {1.4f, 1.7f, 2.7f}, {0.0f, 3.0f, 5.0f}, 1.2f}};
-constexpr float kLaunchUs = 2.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
+constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.9f}, {9.0f}},
+                                  {128, 128, 32, 1, {2.25f}, {3.7f}},
+                                  {64, 64, 32, 2, {1.0f, 1.97f}, {2.1f, 1.8f}, true},
+                                  {32, 32, 64, 2, {0.35f, 0.63f}, {1.2f, 1.6f}, true}};
+constexpr float kLaunchUs = 3.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
+
+// Laying `values` fp32 values out: read, and written as three parts, much of both in the caches.
+float lay_out_us(float values) { return 2.5f + values * 10 / 10e6f; }
 
 // A product's tile, how many of its tiles are one workgroup's, and how many workgroups share the sum of each of the others.
 struct Plan {
     int tile, whole, splits;
     int64_t tiles;
     float us;
+    bool as_is;
 };
 
 float tiles_us(const TileSize& t, float count, float stages, float units) {
@@ -211,27 +219,28 @@ float tiles_us(const TileSize& t, float count, float stages, float units) {
 }
 
 // The fastest by those figures.  A sum is shared out where the last tiles would leave most of the chip idle for longer than a second
-// launch, which adds up what the first left in memory, takes.  k_rows: how many of the two operands run along k; laid-out fp32 ones
-// are read in pieces of 64 bytes then, which takes tiles 5 to 20 % longer (by_rows).
-Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows) {
+// launch, which adds up what the first left in memory, takes.  k_rows: how many of the two operands run along k.
+// lay_out: us for that.
+Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 5, units = compute_units();
-    Plan best = {0, 0, 1, 0, 1e30f};
+    const int64_t narrow = k_rows == 2 ? 4 : k_rows == 1 ? J : std::min<int64_t>(I, J);  // of operands that do not run along k
+    Plan best = {0, 0, 1, 0, 1e30f, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
-        if (tiles > kMostTiles) continue;
-        const float stage = t.depth / 64.f * (dtype == 0 && k_rows == 2 ? t.by_rows : 1.f);
-        const float us = kLaunchUs + tiles_us(t, (float)tiles, k_tiles * stage, (float)units);
-        if (us < best.us) best = {i, (int)tiles, 1, tiles, us};
+        if (tiles > kMostTiles || (t.as_is && narrow < 4)) continue;
+        const float stage = t.depth / 64.f, launch = kLaunchUs + (t.as_is ? 0.f : lay_out);
+        const float us = launch + tiles_us(t, (float)tiles, k_tiles * stage, (float)units);
+        if (us < best.us) best = {i, (int)tiles, 1, tiles, us, t.as_is};
         const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
-        const float base = kLaunchUs + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
+        const float base = launch + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
         if (shared == 0) continue;
         for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / kBytesPerUs;
             if (splits > k_tiles || moved >= best.us || shared * splits > kMostTiles) break;
             const float shared_us = moved + tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units);
-            if (shared_us < best.us) best = {i, (int)whole, splits, tiles, shared_us};
+            if (shared_us < best.us) best = {i, (int)whole, splits, tiles, shared_us, t.as_is};
         }
     }
     return best;
@@ -242,17 +251,18 @@ struct PairPlan {
     int tile, x_splits, w_splits, x_first;
     int64_t x_tiles, w_tiles;
     float us;
+    bool as_is;
 };
 
-PairPlan pair_plan(int dtype, int64_t N, int D, int M) {
+PairPlan pair_plan(int dtype, int64_t N, int D, int M, float lay_out) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 5;
     const float units = (float)compute_units();
-    PairPlan best = {0, 1, 1, 0, 0, 0, 1e30f};
+    PairPlan best = {0, 1, 1, 0, 0, 0, 1e30f, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t x_tiles = ((N + t.i - 1) / t.i) * ((D + t.j - 1) / t.j), w_tiles = ((int64_t)(D + t.i - 1) / t.i) * ((M + t.j - 1) / t.j);
-        if (std::max(x_tiles, w_tiles) > kMostTiles) continue;
+        if (std::max(x_tiles, w_tiles) > kMostTiles || (t.as_is && std::min(D, M) < 4)) continue;
         const float x_stages = (float)((M + t.depth - 1) / t.depth), w_stages = (float)((N + t.depth - 1) / t.depth);
         const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / kBytesPerUs;
         for (const int xs : {1, 2, 4}) {
@@ -260,14 +270,14 @@ PairPlan pair_plan(int dtype, int64_t N, int D, int M) {
             for (const int ws : {1, 2, 4, 8, 16, 32}) {
                 if (ws > 1 && (ws > w_stages || w_tiles * ws > 4 * slots)) break;
                 const float nx = (float)x_tiles * xs, nw = (float)w_tiles * ws;
-                const float kx = std::ceil(x_stages / xs) * unit * t.by_rows, kw = std::ceil(w_stages / ws) * unit;
+                const float kx = std::ceil(x_stages / xs) * unit, kw = std::ceil(w_stages / ws) * unit;
                 // alone as many at once as there are; else the work by the slots, and two fifths of the longer tile for the end
                 const int at_once = std::min((int)std::ceil((nx + nw) / units), t.at_once) - 1;
                 const float x = kx * t.stage[at_once] + t.rest[at_once], w = kw * t.stage[at_once] + t.rest[at_once];
                 float us = std::max(x, w);
                 if (nx + nw > slots) us = std::max(us, (nx * x + nw * w) / slots + 0.4f * std::max(x, w));
-                us += kLaunchUs + (xs > 1 ? kJoinUs + nx * tile_bytes : 0.f) + (ws > 1 ? kJoinUs + nw * tile_bytes : 0.f);
-                if (us < best.us) best = {i, xs, ws, x >= w, x_tiles, w_tiles, us};
+                us += kLaunchUs + (t.as_is ? 0.f : lay_out) + (xs > 1 ? kJoinUs + nx * tile_bytes : 0.f) + (ws > 1 ? kJoinUs + nw * tile_bytes : 0.f);
+                if (us < best.us) best = {i, xs, ws, x >= w, x_tiles, w_tiles, us, t.as_is};
             }
         }
     }
@@ -281,8 +291,6 @@ size_t tile_bytes(int dtype, int tile, int64_t tiles, int splits) {
 
 size_t partial_bytes(int dtype, const Plan& p) { return tile_bytes(dtype, p.tile, p.tiles - p.whole, p.splits); }
 
-// Laying `values` fp32 values out: read, and written as three parts.
-float lay_out_us(float values) { return kLaunchUs + values * 10 / kBytesPerUs; }
 
 ProductArgs product_args(const Operand& A, const Operand& B, int64_t I, int J, int64_t K, int whole, int splits, void* partial,
                          const Epilogue& e) {
@@ -341,7 +349,7 @@ Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t
 
 // What the backward pass has to have laid out, and its products: of both gradients in one launch, or of one.
 struct GradientPlan {
-    bool plain;  // fp32 products of the operands as they are
+    bool plain, as_is;  // fp32 products of the operands as they are: without tiles, or either way
     bool x, w, z, sums, pass, both;
     Plan one;
     PairPlan pair;
@@ -354,21 +362,23 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     g.both = need_dx && need_dw;
     float tiles = 0.f, plain = 0.f;
     const float values = (float)c.N * c.M + (need_dx ? (float)c.D * c.M : 0.f) + (need_dw ? (float)c.N * c.D : 0.f);
-    if (g.both) {
-        g.pair = pair_plan(c.dtype, c.N, c.D, c.M);
-        tiles = g.pair.us, plain = plain_pair_us(c.N, c.D, c.M);
-    } else if (need_dx) {
-        g.one = plan(c.dtype, c.N, c.D, c.M, 2);
-        tiles = g.one.us, plain = plain_f32_us(c.N, c.D, c.M);
-    } else if (need_dw) {
-        g.one = plan(c.dtype, c.D, c.M, c.N, 0);
-        tiles = g.one.us, plain = plain_f32_us(c.D, c.M, c.N);
-    }
     // the pass over G is there for an activation or a bias either way; planes are half as much again to write
-    g.plain = c.dtype == 0 && plain < tiles + lay_out_us(values);
-    g.x = !g.plain && need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
-    g.w = !g.plain && need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
-    g.z = (need_dx || need_dw) && (activation != 0 || (!g.plain && !usable(c.dtype, G, ldg, c.M)));
+    const float lay_out = c.dtype == 0 ? lay_out_us(values) : 0.f;
+    if (g.both) {
+        g.pair = pair_plan(c.dtype, c.N, c.D, c.M, lay_out);
+        tiles = g.pair.us, plain = plain_pair_us(c.N, c.D, c.M), g.as_is = g.pair.as_is;
+    } else if (need_dx) {
+        g.one = plan(c.dtype, c.N, c.D, c.M, 2, lay_out);
+        tiles = g.one.us, plain = plain_f32_us(c.N, c.D, c.M), g.as_is = g.one.as_is;
+    } else if (need_dw) {
+        g.one = plan(c.dtype, c.D, c.M, c.N, 0, lay_out);
+        tiles = g.one.us, plain = plain_f32_us(c.D, c.M, c.N), g.as_is = g.one.as_is;
+    }
+    g.plain = c.dtype == 0 && plain < tiles;
+    g.as_is |= g.plain;
+    g.x = !g.as_is && need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
+    g.w = !g.as_is && need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
+    g.z = (need_dx || need_dw) && (activation != 0 || (!g.as_is && !usable(c.dtype, G, ldg, c.M)));
     g.sums = need_db;
     g.pass = g.z || g.sums;
     share_rows(c.N, c.M, g.slope);
@@ -382,7 +392,7 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
 }
 
 size_t slope_bytes(const DenseCall& c, const GradientPlan& g) {
-    return g.plain ? (size_t)round_up(c.N * c.M * 4, 256) : laid_out_bytes(c.dtype, c.N, c.M);
+    return g.as_is ? (size_t)round_up(c.N * c.M * 4, 256) : laid_out_bytes(c.dtype, c.N, c.M);
 }
 size_t column_bytes(const GradientPlan& g, int M) { return g.sums ? (size_t)round_up((int64_t)g.slope.chunks * M * 4, 256) : 0; }
 
@@ -396,10 +406,10 @@ ForwardPlan forward_plan(const DenseCall& c) {
     ForwardPlan f = {};
     f.few = c.N <= kFewRows;
     if (f.few) return f;
-    f.product = plan(c.dtype, c.N, c.M, c.D, 1);
-    f.plain = c.dtype == 0 && plain_f32_us(c.N, c.M, c.D) < f.product.us + lay_out_us((float)c.N * c.D + (float)c.D * c.M);
-    f.x = !f.plain && !usable(c.dtype, c.X, c.ldx, c.D);
-    f.w = !f.plain && !usable(c.dtype, c.W, c.ldw, c.M);
+    f.product = plan(c.dtype, c.N, c.M, c.D, 1, c.dtype == 0 ? lay_out_us((float)c.N * c.D + (float)c.D * c.M) : 0.f);
+    f.plain = c.dtype == 0 && plain_f32_us(c.N, c.M, c.D) < f.product.us;
+    f.x = !f.plain && !f.product.as_is && !usable(c.dtype, c.X, c.ldx, c.D);
+    f.w = !f.plain && !f.product.as_is && !usable(c.dtype, c.W, c.ldw, c.M);
     return f;
 }
 
@@ -454,7 +464,7 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     if (g.pass) {
         SlopeArgs& a = g.slope;
         a.G = G, a.Z = Z, a.ldg = ldg, a.ldz = ldz, a.N = c.N, a.M = c.M, a.activation = activation;
-        a.to = z, a.plain = g.plain, a.partial = db ? columns : nullptr;
+        a.to = z, a.plain = g.as_is, a.partial = db ? columns : nullptr;
         const hipError_t e = with_type(c.dtype, [&](auto t) {
             hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles) + lay_out_blocks(others)), dim3(256), 0, s,
                                a, others);
@@ -479,6 +489,7 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     }
     const bool f32 = c.dtype == 0;
     const auto gradient = [&](bool k_inner) {
+        if (g.as_is && z) return operand(z, c.M, nullptr, c.N, c.M, k_inner, f32);
         Operand o = operand(G, ldg, z, c.N, c.M, k_inner, f32);
         if (f32 && activation) {
             o.slope_of = static_cast<const float*>(Z), o.activation = activation;

@@ -1,49 +1,33 @@
-// The matrix products of dense linear layers on the matrix cores, C[i][j] = sum_k A(i, k) B(k, j), with the layer's epilogue.
+// The matrix products of dense linear layers on the matrix cores, C[i][j] = sum_k A(i, k) B(k, j), with the layer's epilogue: of
+// 16-bit operands in whole aligned 16-byte units, and of fp32 ones as three planes of bf16 parts, a = h + m + l, a b being
+// l h' + h l' + m m' + m h' + h m' + h h' (split_bf16.h): six products at a sixteenth of the fp32 instructions' cost each.
+//
+// What bounds them is the matrix instructions, and for the largest the power they draw.  16384 x 4096 x 4096 in bf16, us:
+//   X W 395 (1390 TFLOP/s), dZ W^T 402, X^T dZ 393; with the activations of a layer, 16384 x 1024 x 4096, 125, gelu 152, gelu and Z
+//   kept 156 (268 MB written in 31).  fp32, both gradients'
+//   products of 4096 x 768 x 2304, 160 (181 TFLOP/s, of six products 1090).
+// How it gets there, and what was slower:
+//   - Tiles of 256 x 256 by eight wavefronts of 128 x 64: every operand is read from LDS once per 128 or 64 products.  Two
+//     workgroups of 128 x 256 to a compute unit, so that one's epilogue runs beside the other's products: 419 to 500 us, and no
+//     faster at K = 1024.  Instructions of 32 x 32: 425.
+//   - Loads go straight to LDS, a ring of three stages of 32 k; two of 64 k 430 and more.  A stage's barrier lets loads fly on.
+//   - The next step's operands are read from LDS while a step's products run, a read between every two.
+//   - Operands whose rows do not run along k are turned by the LDS reads, so that no layout needs a pass over memory.
+//   - XORed units keep those reads from meeting in a bank.  Tiles go to the XCDs in contiguous ranges, four rows of tiles at a time.
+// Operands of odd strides or addresses are laid out first: loads of them through registers took 1.4 times as long as that and the
+// product.  Which tile, and whether a sum is shared out: dense_linear.hip.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "dense_epilogue.h"
-#include "dense_rows.h"
+#include "dense_tile_f32.h"
 #include "lutnn_kernels.h"
 #include "mfma_tile.h"
 #include "split_bf16.h"
 
 namespace lutnn {
-
-// An operand as the kernel reads it: 16-bit values, rows of `ld` of them in whole aligned 16-byte units, zeros behind a row's end as
-// far as its unit goes; PARTS planes.
-struct Operand {
-    const void* p;
-    int64_t ld, plane;  // values
-    // fp32 operands: where the planes come from, the value at outer index o and k being origin[o * step_outer + k * step_k], times
-    // the activation's slope at slope_of[o * slope_outer + k * slope_k]
-    const float* origin;
-    int64_t step_outer, step_k;
-    const float* slope_of;
-    int64_t slope_outer, slope_k;
-    int activation;
-};
-
-struct ProductArgs {
-    Operand A, B;
-    int64_t I, K;
-    int J, i_tiles, j_tiles;
-    int whole, splits;  // so many tiles are one workgroup's each; `splits` share the sum of each of the others
-    float* partial;     // theirs: [splits][tiles - whole][rows of a tile][columns of it]
-    Epilogue e;
-};
-
-// Both gradients' products in one launch (product::pair_kernel).
-struct PairArgs {
-    ProductArgs x, w;
-    int x_blocks, w_blocks, x_first;  // the blocks are counted at the launch
-    PartialSums sums;
-};
-
 namespace product {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -56,13 +40,6 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, bf16) {
 }
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-
-// Orders the workgroup's LDS operations only: loads to LDS stay in flight.
-__device__ __forceinline__ void lds_barrier() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // What a wavefront's lanes have written to LDS is there for its other lanes.
@@ -175,22 +152,6 @@ struct Tile {
     }
 };
 
-// Workgroup b's tile of `tiles`, -1 for none: consecutive workgroups run on different XCDs, and each of the eight takes a
-// contiguous range.
-__device__ __forceinline__ int of_xcd(int b, int tiles) {
-    const int t = (b & 7) * ((tiles + 7) / 8) + (b >> 3);
-    return t < tiles ? t : -1;
-}
-
-// Where a tile lies: groups of four rows of tiles, column by column, so that neighbours read the same rows and columns.
-struct TilePlace {
-    int i, j;
-};
-__device__ __forceinline__ TilePlace place_of(int tile, int i_tiles, int j_tiles) {
-    const int group = tile / (4 * j_tiles), rest = tile % (4 * j_tiles), rows = min(4, i_tiles - 4 * group);
-    return {4 * group + rest % rows, rest / rows};
-}
-
 // A sum that the parts could not form, as one fp32 chain.
 __device__ __forceinline__ float chain(const ProductArgs& a, int64_t i, int64_t j) {
     const auto value = [](const Operand& o, int64_t outer, int64_t k) {
@@ -203,24 +164,13 @@ __device__ __forceinline__ float chain(const ProductArgs& a, int64_t i, int64_t 
     return sum;
 }
 
-// Asks for the LDS reads of a block between the first `products` of its matrix instructions, in `groups` groups of both.
-template <int reads, int products, int groups, int g = 0>
-__device__ __forceinline__ void interleave() {
-    if constexpr (g < groups) {
-        constexpr int r = reads * (g + 1) / groups - reads * g / groups, m = products * (g + 1) / groups - products * g / groups;
-        if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
-        if constexpr (m > 0) __builtin_amdgcn_sched_group_barrier(0x008, m, 0);
-        interleave<reads, products, groups, g + 1>();
-    }
-}
-
 // A tile's size, wavefronts and ring.  T: the matrices' type; fp32 ones are three planes of bf16 (split_bf16.h).
 template <class T_, int TI_, int TJ_, int WI_, int WJ_, int DEPTH_, int STAGES_>
 struct Config {
     typedef T_ T;
-    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr bool F32 = sizeof(T) == 4, AS_IS = false;
     static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, DEPTH = DEPTH_, STAGES = STAGES_;
-    static constexpr int PARTS = F32 ? 3 : 1, THREADS = 64 * WI * WJ, BUF = (TI + TJ) * DEPTH * 2 * PARTS;
+    static constexpr int PARTS = F32 ? 3 : 1, THREADS = 64 * WI * WJ, WAVES = 2, BUF = (TI + TJ) * DEPTH * 2 * PARTS;
     // the sums on their way out: a wavefront's, ROUND rows at a time
     static constexpr int ROUND = TI / WI < 64 ? TI / WI : 64, COLS = TJ / WJ, PITCH = COLS + 4, OUT = WI * WJ * ROUND * PITCH * 4;
     static constexpr int LDS = STAGES * BUF > OUT ? STAGES * BUF : OUT;
@@ -239,13 +189,10 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
     typedef Tile<TJ, DEPTH, B_K, PARTS, THREADS> TileB;
     static_assert(BUF == TileA::kBytes + TileB::kBytes, "a stage's operands");
 
-    const int whole_blocks = (a.whole + 7) / 8 * 8, shared = a.i_tiles * a.j_tiles - a.whole;
-    const bool is_whole = block < whole_blocks;
-    int tile = is_whole ? of_xcd(block, a.whole) : of_xcd(block - whole_blocks, shared * a.splits);
-    if (tile < 0) return;
-    const int splits = is_whole ? 1 : a.splits, split = is_whole ? 0 : tile / shared, in_shared = is_whole ? 0 : tile % shared;
-    if (!is_whole) tile = a.whole + in_shared;
-    const TilePlace at = place_of(tile, a.i_tiles, a.j_tiles);
+    const Share share = share_of(a, block);
+    if (share.tile < 0) return;
+    const int splits = share.splits, split = share.split;
+    const TilePlace at = place_of(share.tile, a.i_tiles, a.j_tiles);
     const int64_t i0 = (int64_t)at.i * TI;
     const int j0 = at.j * TJ;
 
@@ -469,7 +416,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
                 row[r] = i0 + in_rows + r * STEP;
             }
             if (splits > 1) {
-                float* const to = a.partial + (((int64_t)split * shared + in_shared) * TI + in_rows) * TJ + in_cols;
+                float* const to = a.partial + (share.slot * TI + in_rows) * TJ + in_cols;
 #pragma unroll
                 for (int r = 0; r < BATCH; ++r) store_values(to + r * STEP * TJ, z[r]);
                 continue;
@@ -481,22 +428,30 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
 }
 
 template <class C, bool A_K, bool B_K>
-__global__ __launch_bounds__(C::THREADS) void product_kernel(ProductArgs a) {
+__device__ __forceinline__ void any_tile(const ProductArgs& a, int block, char* const lds) {
+    if constexpr (C::AS_IS)
+        tile_f32<C, A_K, B_K>(a, block, lds);
+    else
+        product_tile<C, A_K, B_K>(a, block, lds);
+}
+
+template <class C, bool A_K, bool B_K>
+__global__ __launch_bounds__(C::THREADS, C::WAVES) void product_kernel(ProductArgs a) {
     __shared__ __align__(1024) char lds[C::LDS];
-    product_tile<C, A_K, B_K>(a, blockIdx.x, lds);
+    any_tile<C, A_K, B_K>(a, blockIdx.x, lds);
 }
 
 // dX = dZ W^T and dW = X^T dZ in one launch, that with the longer tiles first, and db's partial sums added up beside them.
 template <class C>
-__global__ __launch_bounds__(C::THREADS) void pair_kernel(PairArgs p) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES) void pair_kernel(PairArgs p) {
     __shared__ __align__(1024) char lds[C::LDS];
     const int first = p.x_first ? p.x_blocks : p.w_blocks, both = p.x_blocks + p.w_blocks, b = blockIdx.x;
     if (b >= both)
         add_partial_sums<C::THREADS>(p.sums, b - both, lds);
     else if ((b < first) == (p.x_first != 0))
-        product_tile<C, true, true>(p.x, b < first ? b : b - first, lds);
+        any_tile<C, true, true>(p.x, b < first ? b : b - first, lds);
     else
-        product_tile<C, false, false>(p.w, b < first ? b : b - first, lds);
+        any_tile<C, false, false>(p.w, b < first ? b : b - first, lds);
 }
 
 // The shared tiles' sums through the epilogue, four columns per thread.  TI x TJ: a tile.
@@ -584,8 +539,8 @@ hipError_t with_tile(int tile, F&& f) {
         switch (tile) {
             case 0: return f(Config<T, 128, 256, 2, 4, 32, 2>());
             case 1: return f(Config<T, 128, 128, 2, 4, 32, 2>());
-            case 2: return f(Config<T, 64, 128, 2, 2, 32, 2>());
-            default: return f(Config<T, 64, 64, 2, 2, 32, 2>());
+            case 2: return f(ConfigF32<64, 64, 2, 4, 32, 4>());
+            default: return f(ConfigF32<32, 32, 2, 2, 64, 2>());
         }
     } else {
         switch (tile) {

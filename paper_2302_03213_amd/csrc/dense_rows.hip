@@ -83,61 +83,38 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(const T* __restrict_
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// F fragments of an operand, 16 F outer indices from `first` on by 16 k: v[e][r] is the value at k + r, k being the lane group's first,
-// and at the outer index that index_of(e, lane % 16) names: lanes read 16 bytes along k, or F neighbours at each k.
-template <int F, bool K_INNER>
-__device__ __forceinline__ int index_of(int e, int i) {
-    return K_INNER ? 16 * e + i : F * i + e;
-}
-template <int F, bool K_INNER>
-__device__ __forceinline__ void load_fragments(const PlainOperand& o, int64_t first, int64_t count, int64_t k, int64_t K, f32x4 (&v)[F]) {
-    const int i = threadIdx.x & 15;
-    if constexpr (K_INNER) {
-#pragma unroll
-        for (int e = 0; e < F; ++e) {
-            const float* const at = o.p + min(first + 16 * e + i, count - 1) * o.outer;
-            if (k + 4 <= K) {
-                float x[4];
-                load_values(at + k, x);
-                v[e] = f32x4{x[0], x[1], x[2], x[3]};
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[e][r] = k + r < K ? at[k + r] : 0.f;
-            }
-        }
+// A fragment of an operand, 16 outer indices from `first` on, one per lane, by the four k from `k` on.
+template <bool K_INNER>
+__device__ __forceinline__ void load_fragment(const PlainOperand& o, int64_t first, int64_t count, int64_t k, int64_t K, f32x4& v) {
+    const float* const at = o.p + min(first + (threadIdx.x & 15), count - 1) * o.outer;
+    if (K_INNER && k + 4 <= K) {
+        float x[4];
+        load_values(at + k, x);
+        v = f32x4{x[0], x[1], x[2], x[3]};
     } else {
-        const int64_t outer = first + F * i;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float* const at = o.p + min(k + r, K - 1) * o.inner;
-            float x[F];
-            if (outer + F <= count)
-                load_values(at + outer, x);
-            else
-#pragma unroll
-                for (int e = 0; e < F; ++e) x[e] = at[min(outer + e, count - 1)];
-#pragma unroll
-            for (int e = 0; e < F; ++e) v[e][r] = k + r < K ? x[e] : 0.f;
+            const float x = at[min(k + r, K - 1) * o.inner];
+            v[r] = k + r < K ? x : 0.f;
         }
     }
 }
 
-// 16 FI rows by 16 FJ columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth
-// 16 k, two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of
-// both operands, and instruction r takes the r-th of each.  Blocks: row blocks * column blocks, row block fastest.
+// 16 rows by 16 columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth 16 k,
+// two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of both
+// operands, and instruction r takes the r-th of each.  Blocks: row blocks * column blocks, row block fastest.  What bounds it is
+// the memory's latency, a launch's included: 37 x 768 x 768 6 us, 7 of them the tiles'; 64 x 768 x 768 both 7 and 9.
 struct PlainArgs {
     PlainOperand A, B;
     int64_t I, K;
     int J, row_blocks, col_blocks;
     Epilogue e;
 };
-template <int FI, int FJ>
 struct PlainShared {
-    float part[kWaves][FI * 16][16 * FJ + 1];
+    float part[kWaves][16][17];
 };
-template <int FI, int FJ, bool A_K, bool B_K>
-__device__ __forceinline__ void plain_f32_block(const PlainArgs& args, int index, PlainShared<FI, FJ>& shared) {
-    constexpr int COLS = 16 * FJ;
+template <bool A_K, bool B_K>
+__device__ __forceinline__ void plain_f32_block(const PlainArgs& args, int index, PlainShared& shared) {
     auto& part = shared.part;
     const PlainOperand &A = args.A, &B = args.B;
     const int64_t I = args.I, K = args.K;
@@ -145,25 +122,21 @@ __device__ __forceinline__ void plain_f32_block(const PlainArgs& args, int index
     const Epilogue& e = args.e;
     const int block = strip_of(index, row_blocks * args.col_blocks);
     if (block < 0) return;
-    const int64_t i0 = (int64_t)(block % row_blocks) * FI * 16;
-    const int j0 = block / row_blocks * COLS;
+    const int64_t i0 = (int64_t)(block % row_blocks) * 16;
+    const int j0 = block / row_blocks * 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, q = lane >> 4;
-    f32x4 sum[FI][FJ] = {};
+    f32x4 sum = {};
     struct Chunk {
-        f32x4 a[FI], b[FJ];
+        f32x4 a, b;
     };
     const auto load = [&](Chunk& c, int64_t k) {
         if (k >= K) return;
-        load_fragments<FJ, B_K>(B, j0, J, k + 4 * q, K, c.b);
-        load_fragments<FI, A_K>(A, i0, I, k + 4 * q, K, c.a);
+        load_fragment<B_K>(B, j0, J, k + 4 * q, K, c.b);
+        load_fragment<A_K>(A, i0, I, k + 4 * q, K, c.a);
     };
     const auto multiply = [&](const Chunk& c) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < FI; ++i)
-#pragma unroll
-                for (int j = 0; j < FJ; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(c.b[j][r], c.a[i][r], sum[i][j], 0, 0, 0);
+        for (int r = 0; r < 4; ++r) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(c.b[r], c.a[r], sum, 0, 0, 0);
     };
     constexpr int STEP = 16 * kWaves;
     Chunk one, two;
@@ -183,103 +156,49 @@ __device__ __forceinline__ void plain_f32_block(const PlainArgs& args, int index
     }
     // the first operand's index is the instruction's row: a lane has columns 4 q .. 4 q + 3 of row i16
 #pragma unroll
-    for (int i = 0; i < FI; ++i)
-#pragma unroll
-        for (int j = 0; j < FJ; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) part[wave][index_of<FI, A_K>(i, i16)][index_of<FJ, B_K>(j, 4 * q + r)] = sum[i][j][r];
+    for (int r = 0; r < 4; ++r) part[wave][i16][4 * q + r] = sum[r];
     __syncthreads();
-    for (int v = threadIdx.x; v < FI * 16 * COLS; v += kThreads) {
-        const int64_t row[1] = {i0 + v / COLS};
-        const int col = j0 + v % COLS;
-        if (row[0] >= I || col >= J) continue;
-        float z[1][1] = {{0.f}}, bias[1];
+    const int v = threadIdx.x, col = j0 + v % 16;
+    const int64_t row[1] = {i0 + v / 16};
+    if (v >= 256 || row[0] >= I || col >= J) return;
+    float z[1][1] = {{0.f}}, bias[1];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) z[0][0] += part[w][v / COLS][v % COLS];
-        load_bias(e, col, J, bias);
-        finish<float>(e, row, col, I, J, bias, z);
-    }
+    for (int w = 0; w < kWaves; ++w) z[0][0] += part[w][v / 16][v % 16];
+    load_bias(e, col, J, bias);
+    finish<float>(e, row, col, I, J, bias, z);
 }
 
-template <int FI, int FJ, bool A_K, bool B_K>
+template <bool A_K, bool B_K>
 __global__ __launch_bounds__(kThreads) void plain_f32_kernel(PlainArgs a) {
-    __shared__ PlainShared<FI, FJ> shared;
-    plain_f32_block<FI, FJ, A_K, B_K>(a, blockIdx.x, shared);
+    __shared__ PlainShared shared;
+    plain_f32_block<A_K, B_K>(a, blockIdx.x, shared);
 }
 
 // Both gradients' products in one launch, and db's partial sums.
-template <int FI, int FJ>
 __global__ __launch_bounds__(kThreads) void plain_pair_kernel(PlainArgs x, PlainArgs w, int x_blocks, int w_blocks, PartialSums sums) {
-    __shared__ __align__(8) PlainShared<FI, FJ> shared;
+    __shared__ __align__(8) PlainShared shared;
     const int b = blockIdx.x;
     if (b >= x_blocks + w_blocks)
         add_partial_sums<kThreads>(sums, b - x_blocks - w_blocks, &shared);
     else if (b < x_blocks)
-        plain_f32_block<FI, FJ, true, true>(x, b, shared);
+        plain_f32_block<true, true>(x, b, shared);
     else
-        plain_f32_block<FI, FJ, false, false>(w, b - x_blocks, shared);
+        plain_f32_block<false, false>(w, b - x_blocks, shared);
 }
 
-// Fragments of rows and of columns per workgroup, and what a round of workgroups, one per compute unit, takes per k and beside that, in us: the three
-// layouts' average over products of 37 x 768 to 2048 x 2048.  (Four by four spill.)
-struct Block {
-    int fi, fj;
-    float per_k, rest;
-};
-constexpr Block kBlocks[] = {{1, 1, 0.0032f, 0.6f}, {2, 2, 0.0075f, 1.2f}, {4, 2, 0.0128f, 1.8f}};
-
-float blocks_of(const Block& b, int64_t I, int J) {
-    return (float)((I + 16 * b.fi - 1) / (16 * b.fi)) * (float)((J + 16 * b.fj - 1) / (16 * b.fj));
-}
-
-// A launch, and rounds of workgroups.
-float block_us(const Block& b, int64_t I, int J, int64_t K, float units) {
-    if (blocks_of(b, I, J) > kMostTiles) return 1e30f;
-    return 3.f + std::ceil(blocks_of(b, I, J) / units) * (K * b.per_k + b.rest);
-}
-
-// ... of both gradients': of workgroups of two kinds
-float pair_us(const Block& b, int64_t N, int D, int M, float units) {
-    if (std::max(blocks_of(b, N, D), blocks_of(b, D, M)) > kMostTiles) return 1e30f;
-    const float x = M * b.per_k + b.rest, w = N * b.per_k + b.rest;
-    return 3.f + std::max(std::max(x, w), (blocks_of(b, N, D) * x + blocks_of(b, D, M) * w) / units + 0.5f * std::min(x, w));
-}
-
-template <class Us>
-int best_block(Us&& us) {
-    int best = 0;
-    for (int i = 1; i < (int)(sizeof(kBlocks) / sizeof(kBlocks[0])); ++i)
-        if (us(kBlocks[i]) < us(kBlocks[best])) best = i;
-    return best;
-}
-int best_block(int64_t I, int J, int64_t K) {
-    const float units = (float)compute_units();
-    return best_block([&](const Block& b) { return block_us(b, I, J, K, units); });
-}
-int best_pair(int64_t N, int D, int M) {
-    const float units = (float)compute_units();
-    return best_block([&](const Block& b) { return pair_us(b, N, D, M, units); });
-}
-
-// Calls f with the fragments of a block.
-template <class F>
-hipError_t with_block(int block, F&& f) {
-    using std::integral_constant;
-    switch (block) {
-        case 0: return f(integral_constant<int, 1>(), integral_constant<int, 1>());
-        case 1: return f(integral_constant<int, 2>(), integral_constant<int, 2>());
-        default: return f(integral_constant<int, 4>(), integral_constant<int, 2>());
-    }
-}
+int64_t blocks_of(int64_t I, int J) { return ((I + 15) / 16) * ((J + 15) / 16); }
 
 // Sets the blocks; how many workgroups they take, 0 for too many.
-template <int FI, int FJ>
 int count_blocks(PlainArgs& a) {
-    const int64_t rows = (a.I + 16 * FI - 1) / (16 * FI), cols = (a.J + 16 * FJ - 1) / (16 * FJ);
-    if (rows * cols > kMostTiles) return 0;
-    a.row_blocks = (int)rows, a.col_blocks = (int)cols;
-    return (int)(rows * cols + 7) / 8 * 8;
+    const int64_t blocks = blocks_of(a.I, a.J);
+    if (blocks > kMostTiles) return 0;
+    a.row_blocks = (int)((a.I + 15) / 16), a.col_blocks = (a.J + 15) / 16;
+    return (int)(blocks + 7) / 8 * 8;
 }
+
+// What a round of workgroups, one per compute unit, takes per k and beside that, in us: the three layouts' average over products of
+// 8 x 768 x 768 to 128 x 768 x 2304.
+constexpr float kLaunchUs = 4.2f, kPerK = 0.0032f, kRest = 0.2f;
 
 }  // namespace
 
@@ -299,36 +218,39 @@ hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, con
 }
 
 hipError_t launch_plain_f32(const PlainOperand& A, const PlainOperand& B, int64_t I, int J, int64_t K, const Epilogue& e, hipStream_t s) {
-    return with_block(best_block(I, J, K), [&](auto fi, auto fj) {
-        constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
-        PlainArgs a = {A, B, I, K, J, 0, 0, e};
-        const int blocks = count_blocks<FI, FJ>(a);
-        if (blocks == 0) return hipErrorInvalidConfiguration;
-        if (A.inner != 1)
-            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, false, false>), dim3(blocks), dim3(kThreads), 0, s, a);
-        else if (B.inner == 1)
-            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, true, true>), dim3(blocks), dim3(kThreads), 0, s, a);
-        else
-            hipLaunchKernelGGL((plain_f32_kernel<FI, FJ, true, false>), dim3(blocks), dim3(kThreads), 0, s, a);
-        return hipGetLastError();
-    });
+    PlainArgs a = {A, B, I, K, J, 0, 0, e};
+    const int blocks = count_blocks(a);
+    if (blocks == 0) return hipErrorInvalidConfiguration;
+    if (A.inner != 1)
+        hipLaunchKernelGGL((plain_f32_kernel<false, false>), dim3(blocks), dim3(kThreads), 0, s, a);
+    else if (B.inner == 1)
+        hipLaunchKernelGGL((plain_f32_kernel<true, true>), dim3(blocks), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((plain_f32_kernel<true, false>), dim3(blocks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
 }
 
-float plain_f32_us(int64_t I, int J, int64_t K) { return block_us(kBlocks[best_block(I, J, K)], I, J, K, (float)compute_units()); }
+float plain_f32_us(int64_t I, int J, int64_t K) {
+    const int64_t blocks = blocks_of(I, J);
+    return blocks > kMostTiles ? 1e30f : kLaunchUs + std::ceil((float)blocks / compute_units()) * (K * kPerK + kRest);
+}
 
 hipError_t launch_plain_pair_f32(const float* dZ, int64_t ldg, const float* W, int64_t ldw, const float* X, int64_t ldx, int64_t N, int D,
                                  int M, const Epilogue& to_x, const Epilogue& to_w, const PartialSums& sums, hipStream_t s) {
-    return with_block(best_pair(N, D, M), [&](auto fi, auto fj) {
-        constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
-        PlainArgs x = {{dZ, ldg, 1}, {W, ldw, 1}, N, M, D, 0, 0, to_x}, w = {{X, 1, ldx}, {dZ, 1, ldg}, D, N, M, 0, 0, to_w};
-        const int x_blocks = count_blocks<FI, FJ>(x), w_blocks = count_blocks<FI, FJ>(w);
-        if (x_blocks == 0 || w_blocks == 0) return hipErrorInvalidConfiguration;
-        const unsigned blocks = x_blocks + w_blocks + (sums.out ? (sums.width + 31) / 32 : 0);
-        hipLaunchKernelGGL((plain_pair_kernel<FI, FJ>), dim3(blocks), dim3(kThreads), 0, s, x, w, x_blocks, w_blocks, sums);
-        return hipGetLastError();
-    });
+    PlainArgs x = {{dZ, ldg, 1}, {W, ldw, 1}, N, M, D, 0, 0, to_x}, w = {{X, 1, ldx}, {dZ, 1, ldg}, D, N, M, 0, 0, to_w};
+    const int x_blocks = count_blocks(x), w_blocks = count_blocks(w);
+    if (x_blocks == 0 || w_blocks == 0) return hipErrorInvalidConfiguration;
+    const unsigned blocks = x_blocks + w_blocks + (sums.out ? (sums.width + 31) / 32 : 0);
+    hipLaunchKernelGGL(plain_pair_kernel, dim3(blocks), dim3(kThreads), 0, s, x, w, x_blocks, w_blocks, sums);
+    return hipGetLastError();
 }
 
-float plain_pair_us(int64_t N, int D, int M) { return pair_us(kBlocks[best_pair(N, D, M)], N, D, M, (float)compute_units()); }
+// of workgroups of two kinds
+float plain_pair_us(int64_t N, int D, int M) {
+    const int64_t x_blocks = blocks_of(N, D), w_blocks = blocks_of(D, M);
+    if (std::max(x_blocks, w_blocks) > kMostTiles) return 1e30f;
+    const float x = M * kPerK + kRest, w = N * kPerK + kRest;
+    return kLaunchUs + std::max(std::max(x, w), ((float)x_blocks * x + (float)w_blocks * w) / compute_units() + 1.2f * std::min(x, w));
+}
 
 }  // namespace lutnn

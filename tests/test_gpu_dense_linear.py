@@ -91,6 +91,28 @@ def test_large(lut, N, D, M, kind):
                     du.check(g, want, off)
 
 
+# fp32 of some hundred rows, and larger ones of odd widths: tiles that end early on either side and in k, widths around four
+MIDDLE = [(300, 65, 67), (1000, 100, 300), (257, 129, 5), (500, 5, 129), (700, 4, 4), (600, 3, 900), (600, 900, 3), (65, 1000, 1001),
+          (2000, 33, 1), (90, 4100, 260), (2050, 1001, 1003), (4099, 1003, 1801)]
+
+
+@pytest.mark.parametrize("pad", [0, 1])
+@pytest.mark.parametrize("N,D,M", MIDDLE)
+def test_middle_sizes_in_fp32(lut, N, D, M, pad):
+    X, W, b, R, G = operands(N, D, M, torch.float32, seed=N + D + M)
+    if pad:
+        X, W, R, G = (du.strided(t, pad, 1) for t in (X, W, R, G))
+    Y = lut.dense_linear(X, W, b, "gelu", R)
+    du.check(Y, *du.dense64(X, W, b, "gelu", R)[:2])
+    for activation in (None, "gelu"):
+        wanted = du.dense_backward64(X, W, G, R, activation)
+        for needs in ((True, True, True), (True, False, False), (False, True, False)):
+            got = lut.dense_linear_backward(X, W, G, R if activation else None, activation, *needs)
+            for g, (want, off) in zip(got, wanted):
+                if g is not None:
+                    du.check(g, want, off)
+
+
 @pytest.mark.parametrize("needs", list(itertools.product((False, True), repeat=3)))
 def test_what_is_not_needed_changes_nothing(lut, needs):
     X, W, _, _, G = operands(70, 136, 72, torch.bfloat16, seed=3)
