@@ -1,5 +1,5 @@
 // Dense layers of few rows: what bounds them is reading W once and the launch itself, so each is one launch that reads its operands
-// as they are.
+// as they are.  1 x 1024 x 4096 in bf16 4.7 us, 8.4 MB at 1.8 TB/s; 37 x 768 x 768 in fp32 5.8.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -103,7 +103,7 @@ __device__ __forceinline__ void load_fragment(const PlainOperand& o, int64_t fir
 // 16 rows by 16 columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth 16 k,
 // two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of both
 // operands, and instruction r takes the r-th of each.  Blocks: row blocks * column blocks, row block fastest.  What bounds it is
-// the memory's latency, a launch's included: 37 x 768 x 768 6 us, 7 of them the tiles'; 64 x 768 x 768 both 7 and 9.
+// latency: 37 x 768 x 768 5.8 us, where the tiles of dense_tile_f32.h take 8.6; from 128 rows on those are as fast.
 struct PlainArgs {
     PlainOperand A, B;
     int64_t I, K;
