@@ -30,9 +30,9 @@ __device__ __forceinline__ float activate(float z, int activation) {
     switch (activation) {
         case kActRelu: return z < 0.f ? 0.f : z;
         case kActGelu: {
-            float density;  // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+            float density;  // z Phi(z) = max(z, 0) - |z| Phi(-|z|), where the last is a zero long before |z| reaches 100
             const float tail = normal_tail(z, density);
-            return __fmaf_rn(-fabsf(z), tail, fmaxf(z, 0.f));
+            return __fmaf_rn(-fminf(fabsf(z), 100.f), tail, fmaxf(z, 0.f));
         }
         case kActGeluTanh: return z * logistic(kGeluTanhScale * z * (1.f + kGeluTanhCubic * z * z));
         case kActSilu: return z * logistic(z);
@@ -40,7 +40,9 @@ __device__ __forceinline__ float activate(float z, int activation) {
     }
 }
 
+// Far from zero 0 or 1, also where a product below would be of an infinite z, or z * z, and a zero.
 __device__ __forceinline__ float slope(float z, int activation) {
+    if (fabsf(z) > (activation == kActSilu ? 90.f : 30.f)) return z > 0.f ? 1.f : 0.f;
     switch (activation) {
         case kActRelu: return z > 0.f ? 1.f : 0.f;
         case kActGelu: {
@@ -49,7 +51,6 @@ __device__ __forceinline__ float slope(float z, int activation) {
             return __fmaf_rn(z * 0.3989422804014327f, density, z < 0.f ? tail : 1.f - tail);
         }
         case kActGeluTanh: {
-            if (fabsf(z) > 30.f) return z > 0.f ? 1.f : 0.f;  // where z * z may overflow against a zero
             const float zz = z * z, s = logistic(kGeluTanhScale * z * (1.f + kGeluTanhCubic * zz));
             return s + z * s * (1.f - s) * kGeluTanhScale * (1.f + 3.f * kGeluTanhCubic * zz);
         }

@@ -177,6 +177,32 @@ def test_values_that_are_not_finite_stay_where_they_belong(lut, kind):
             assert torch.isnan(g).equal(torch.isnan(want)) and torch.isinf(g).equal(torch.isinf(want))
 
 
+@pytest.mark.parametrize("kind", list(du.TYPES))
+@pytest.mark.parametrize("N", [3, 40, 700])
+def test_activations_far_from_zero(lut, N, kind):
+    """Infinite, missing and very large preactivations, on the way there and back."""
+    T = du.TYPES[kind]
+    far = [float("inf"), float("nan"), 6e4, 110.0, 31.0, 6.0, -6.0, -31.0, -110.0, -6e4] + ([1e30, -1e30] if kind != "f16" else [])
+    X = torch.tensor((far * N)[:N * 4], dtype=T, device="cuda").view(-1, 1)
+    W = torch.ones((1, 8), dtype=T, device="cuda")
+    wide = X.expand(-1, 8).contiguous()
+    G = torch.ones_like(wide)
+    minus = wide.clone()
+    minus[torch.isposinf(minus)] = float("-inf")
+    for activation in du.ACTIVATIONS[1:]:
+        Y, want = lut.dense_linear(X, W, None, activation), du.act64(wide.double(), activation)
+        assert torch.isnan(Y).equal(torch.isnan(want)) and torch.isinf(Y).equal(torch.isinf(want.to(T)))
+        fine = torch.isfinite(want.to(T))
+        du.check(Y[fine], want[fine], 2.0 ** -20 * (want[fine].abs() + 1) + du.half(T) * want[fine].abs() + du.smallest(T))
+        for Z in (wide, minus):
+            db = lut.dense_linear_backward(X, W, G, Z, activation)[2]
+            assert torch.isnan(db).all() == bool(activation != "relu" and torch.isnan(Z).any())
+            some = ~torch.isnan(Z[:, 0])
+            _, _, db = lut.dense_linear_backward(X[some], W, G[some], Z[some], activation)
+            limits = torch.where(torch.isinf(Z), (Z > 0).double(), du.slope64(Z.double().clamp(-1e4, 1e4), activation))[some]
+            du.check(db, limits.sum(0), 2.0 ** -18 * limits.abs().sum(0) + 2.0 ** -20 * len(limits))
+
+
 def test_fp32_values_of_any_size(lut):
     """Very large and very small operands keep the precision of fp32 products."""
     for exponent in (-50, -30, 30, 50):
