@@ -180,7 +180,7 @@ hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db
 // 64 k, and beside that.  16 bits: from products of 16 x 16 n tiles at K = 512 and 2560, the three layouts' average.  Small tiles are
 // bound by what a compute unit gets from L2 (75 GB/s), the large ones by the matrix instructions and the power they draw.  fp32: fitted
 // to the times of 28 sizes from 8 x 768 x 768 to 4096 x 4096 x 768, three products each, which they then order so that the choice
-// takes 1.2 % longer than the best of all; tiles of 64 x 64 and 64 x 128 from planes were the best of none by more than 1 %.
+// takes 2 % longer than the best of all; tiles of 64 x 64 and 64 x 128 from planes were the best of none by more than 1 %.
 struct TileSize {
     int i, j, depth, at_once;
     float stage[4], rest[4];
@@ -191,10 +191,10 @@ constexpr TileSize kTiles16[] = {{256, 256, 32, 1, {1.55f}, {9.0f}},
                                  {64, 128, 64, 2, {0.61f, 0.65f}, {0.5f, 2.5f}},
                                  {64, 64, 64, 3, {0.23f, 0.46f, 0.66f}, {1.0f, 0.7f, 1.0f}},
                                  {32, 64, 64, 4, {0.16f, 0.37f, 0.56f, 0.72f}, {1.0f, 0.5f, 0.5f, 0.5f}}};
-constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.9f}, {9.0f}},
-                                  {128, 128, 32, 1, {2.25f}, {3.7f}},
-                                  {64, 64, 32, 2, {1.0f, 1.97f}, {2.1f, 1.8f}, true},
-                                  {32, 32, 64, 2, {0.35f, 0.63f}, {1.2f, 1.6f}, true}};
+constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.3f}, {8.4f}},
+                                  {128, 128, 32, 1, {2.02f}, {3.7f}},
+                                  {64, 64, 32, 2, {1.08f, 2.07f}, {1.5f, 1.7f}, true},
+                                  {32, 32, 32, 2, {0.32f, 0.56f}, {0.8f, 0.8f}, true}};
 constexpr float kLaunchUs = 3.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
 
 // Laying `values` fp32 values out: read, and written as three parts, much of both in the caches.
@@ -231,7 +231,10 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
         if (tiles > kMostTiles || (t.as_is && narrow < 4)) continue;
         const float stage = t.depth / 64.f, launch = kLaunchUs + (t.as_is ? 0.f : lay_out);
-        const float us = launch + tiles_us(t, (float)tiles, k_tiles * stage, (float)units);
+        // what tiles that read their operands as they are have on its way: 2 us for two stages of every workgroup
+        const float bytes = t.as_is ? (float)(I + J) * K * 4 : 0.f, slots_bytes = (t.i + t.j) * t.depth * 4.f;
+        const auto memory_us = [&](float workgroups) { return bytes / (std::min(workgroups, (float)units * t.at_once) * slots_bytes); };
+        const float us = launch + std::max(tiles_us(t, (float)tiles, k_tiles * stage, (float)units), memory_us((float)tiles));
         if (us < best.us) best = {i, (int)tiles, 1, tiles, us, t.as_is};
         const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
         const float base = launch + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
@@ -239,7 +242,8 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
         for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / kBytesPerUs;
             if (splits > k_tiles || moved >= best.us || shared * splits > kMostTiles) break;
-            const float shared_us = moved + tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units);
+            const float shared_us = moved + std::max(tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units),
+                                                     memory_us((float)tiles + (float)shared * (splits - 1)));
             if (shared_us < best.us) best = {i, (int)whole, splits, tiles, shared_us, t.as_is};
         }
     }

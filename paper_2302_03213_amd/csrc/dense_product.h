@@ -540,7 +540,7 @@ hipError_t with_tile(int tile, F&& f) {
             case 0: return f(Config<T, 128, 256, 2, 4, 32, 2>());
             case 1: return f(Config<T, 128, 128, 2, 4, 32, 2>());
             case 2: return f(ConfigF32<64, 64, 2, 4, 32, 4>());
-            default: return f(ConfigF32<32, 32, 2, 2, 64, 2>());
+            default: return f(ConfigF32<32, 32, 2, 2, 32, 4>());
         }
     } else {
         switch (tile) {

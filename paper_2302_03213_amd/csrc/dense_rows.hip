@@ -103,7 +103,7 @@ __device__ __forceinline__ void load_fragment(const PlainOperand& o, int64_t fir
 // 16 rows by 16 columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth 16 k,
 // two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of both
 // operands, and instruction r takes the r-th of each.  Blocks: row blocks * column blocks, row block fastest.  What bounds it is
-// latency: 37 x 768 x 768 5.8 us, where the tiles of dense_tile_f32.h take 8.6; from 128 rows on those are as fast.
+// latency: 37 x 768 x 768 5.6 us, where the tiles of dense_tile_f32.h take 7.4; from 128 rows on those are as fast.
 struct PlainArgs {
     PlainOperand A, B;
     int64_t I, K;
@@ -198,7 +198,7 @@ int count_blocks(PlainArgs& a) {
 
 // What a round of workgroups, one per compute unit, takes per k and beside that, in us: the three layouts' average over products of
 // 8 x 768 x 768 to 128 x 768 x 2304.
-constexpr float kLaunchUs = 4.2f, kPerK = 0.0032f, kRest = 0.2f;
+constexpr float kLaunchUs = 2.6f, kPerK = 0.0033f, kRest = 0.27f;
 
 }  // namespace
 
@@ -250,7 +250,7 @@ float plain_pair_us(int64_t N, int D, int M) {
     const int64_t x_blocks = blocks_of(N, D), w_blocks = blocks_of(D, M);
     if (std::max(x_blocks, w_blocks) > kMostTiles) return 1e30f;
     const float x = M * kPerK + kRest, w = N * kPerK + kRest;
-    return kLaunchUs + std::max(std::max(x, w), ((float)x_blocks * x + (float)w_blocks * w) / compute_units() + 1.2f * std::min(x, w));
+    return kLaunchUs + std::max(std::max(x, w), ((float)x_blocks * x + (float)w_blocks * w) / compute_units() + 1.4f * std::min(x, w));
 }
 
 }  // namespace lutnn

@@ -2,10 +2,12 @@
 // dense_product.h out takes longer than their faster products save.
 //
 // What bounds it is the instructions, 614 GFLOP/s a compute unit: a 64 x 64 tile by 32 k takes 0.48 us of 0.43.  256 x 768 x 768
-// 8.9 us (planes 17; straight from memory 11 to 16), 1024 x 768 x 768 17.5 (planes 28), 256 x 2048 x 2048 26 (planes 32); from
-// 2048 x 1024 x 1024 (both 39) on the planes are faster.  Values go through registers to LDS, four stages ahead, so that rows of
-// any alignment are read 16 bytes at a time; a stage's operands are read from LDS while the last one's products run (18 % faster than behind its
-// barrier, for the 64 x 64 tile).  Wider tiles leave too few workgroups where this is used.
+// 7.7 us (planes 20; straight from memory 10.7), 1024 x 768 x 768 15 (planes 29), 256 x 2048 x 2048 23 (planes 32); from
+// 2048 x 1024 x 1024 (39 and 40) on the planes are faster.  Values go through registers to LDS, two stages ahead of that, so that
+// rows of any alignment are read 16 bytes at a time: four stages took 8 % longer, a third of it the first loads, but for a few
+// rows by a W past the caches (64 x 4096 x 4096 26 us for 34; the sum is shared out there, 25).  A stage's operands are read from LDS
+// while the last one's products run (18 % faster than behind its barrier, for the 64 x 64 tile).  Wider tiles leave too few
+// workgroups where this is used; 64 x 32 is no faster than 32 x 32.
 #pragma once
 #include <type_traits>
 
@@ -94,11 +96,11 @@ struct ConfigF32 {
     static constexpr int LDS = 2 * 4 * (floats(TI) + floats(TJ));
 };
 
-// Workgroup `block`'s tile.  Stage t + 1's operands are read from LDS, stage t + 2's written there and stage t + 6's asked for while
+// Workgroup `block`'s tile.  Stage t + 1's operands are read from LDS, stage t + 2's written there and stage t + 4's asked for while
 // stage t's are multiplied.
 template <class C, bool A_K, bool B_K>
 __device__ __forceinline__ void tile_f32(const ProductArgs& a, int block, char* const lds) {
-    constexpr int TI = C::TI, TJ = C::TJ, DEPTH = C::DEPTH, FI = TI / C::WI / 16, FJ = TJ / C::WJ / 16, AHEAD = 4, STEPS = DEPTH / 16;
+    constexpr int TI = C::TI, TJ = C::TJ, DEPTH = C::DEPTH, FI = TI / C::WI / 16, FJ = TJ / C::WJ / 16, AHEAD = 2, STEPS = DEPTH / 16;
     typedef Panel<TI, DEPTH, A_K, C::THREADS> PanelA;
     typedef Panel<TJ, DEPTH, B_K, C::THREADS> PanelB;
     constexpr int BUF = PanelA::kFloats + PanelB::kFloats;
