@@ -18,6 +18,7 @@ namespace lutnn {
 namespace {
 
 constexpr int kVec = 8;                      // columns per thread of the passes over a matrix
+constexpr int64_t kDirectRows = 2048;        // of a bias' gradient that has no pass of its own
 constexpr int64_t kMaxStride = 1 << 21;      // values: a tile's rows within 32-bit offsets
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -354,7 +355,7 @@ Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t
 // What the backward pass has to have laid out, and its products: of both gradients in one launch, or of one.
 struct GradientPlan {
     bool plain, as_is;  // fp32 products of the operands as they are: without tiles, or either way
-    bool x, w, z, sums, pass, both;
+    bool x, w, z, sums, direct, pass, both;  // direct: db's sums are taken beside the products
     Plan one;
     PairPlan pair;
     SlopeArgs slope;
@@ -383,7 +384,10 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     g.x = !g.as_is && need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
     g.w = !g.as_is && need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
     g.z = (need_dx || need_dw) && (activation != 0 || (!g.as_is && !usable(c.dtype, G, ldg, c.M)));
-    g.sums = need_db;
+    // Where nothing else has to read G before the products, few rows of it are added up beside them, 32 columns per workgroup, and
+    // not in a pass of their own: 256 x 768 x 768 in bf16 8.0 us for 12.0, 2048 x 768 x 768 22.7 for 23.2, 4096 x 256 x 256 23.4 for 18.3.
+    g.direct = need_db && g.both && !g.z && !g.x && !g.w && c.N <= kDirectRows;
+    g.sums = need_db && !g.direct;
     g.pass = g.z || g.sums;
     share_rows(c.N, c.M, g.slope);
     if (!g.plain && g.both) {
@@ -468,7 +472,7 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     if (g.pass) {
         SlopeArgs& a = g.slope;
         a.G = G, a.Z = Z, a.ldg = ldg, a.ldz = ldz, a.N = c.N, a.M = c.M, a.activation = activation;
-        a.to = z, a.plain = g.as_is, a.partial = db ? columns : nullptr;
+        a.to = z, a.plain = g.as_is, a.partial = g.sums ? columns : nullptr;
         const hipError_t e = with_type(c.dtype, [&](auto t) {
             hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles) + lay_out_blocks(others)), dim3(256), 0, s,
                                a, others);
@@ -478,7 +482,7 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     } else if (hipError_t e = launch_lay_out(c.dtype, others, s)) {
         return e;
     }
-    const PartialSums sums = {columns, g.slope.chunks, c.M, db};
+    const PartialSums sums = g.direct ? PartialSums{nullptr, (int)c.N, c.M, db, G, ldg} : PartialSums{columns, g.slope.chunks, c.M, db, nullptr, 0};
     if (!g.both && db)
         if (hipError_t e = launch_partial_sums(columns, g.slope.chunks, c.M, c.M, db, nullptr, s)) return e;
     if (!dX && !dW) return hipSuccess;

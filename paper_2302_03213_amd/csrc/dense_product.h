@@ -447,7 +447,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES) void pair_kernel(PairArgs p) 
     __shared__ __align__(1024) char lds[C::LDS];
     const int first = p.x_first ? p.x_blocks : p.w_blocks, both = p.x_blocks + p.w_blocks, b = blockIdx.x;
     if (b >= both)
-        add_partial_sums<C::THREADS>(p.sums, b - both, lds);
+        add_partial_sums<typename C::T, C::THREADS>(p.sums, b - both, lds);
     else if ((b < first) == (p.x_first != 0))
         any_tile<C, true, true>(p.x, b < first ? b : b - first, lds);
     else

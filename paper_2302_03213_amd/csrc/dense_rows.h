@@ -14,23 +14,33 @@ constexpr int kFewRows = 4;
 hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int D, int M,
                            const Epilogue& e, hipStream_t s);
 
-// fp32 sums that a kernel's workgroups left, [count][width], to be added up by workgroups of a later launch; no `out`: none.
+// Rows to be added up by workgroups of a launch beside other work: fp32 sums that an earlier kernel's workgroups left,
+// [count][width], or a matrix of the launch's type itself, row stride ld; no `out`: none.
 struct PartialSums {
     const float* partial;
     int count, width;
     float* out;
+    const void* matrix;
+    int64_t ld;
 };
 
 // 32 columns of them by workgroup `block` of THREADS, 64-bit sums in a fixed order.  lds: THREADS / 32 * 33 doubles.
-template <int THREADS>
+template <class T, int THREADS>
 __device__ __forceinline__ void add_partial_sums(const PartialSums& p, int block, void* lds) {
     constexpr int GROUPS = THREADS / 32;
     double(*const part)[33] = static_cast<double(*)[33]>(lds);
     const int i = threadIdx.x & 31, group = threadIdx.x >> 5, m = block * 32 + i;
     double sum = 0;
-    if (m < p.width)
+    const auto add = [&](const auto* from, int64_t ld) {
 #pragma unroll 8
-        for (int k = group; k < p.count; k += GROUPS) sum += p.partial[(int64_t)k * p.width + m];
+        for (int k = group; k < p.count; k += GROUPS) sum += (float)from[k * ld + m];
+    };
+    if (m < p.width) {
+        if (p.matrix)
+            add(static_cast<const T*>(p.matrix), p.ld);
+        else
+            add(p.partial, p.width);
+    }
     part[group][i] = sum;
     __syncthreads();
     if (group != 0 || m >= p.width) return;

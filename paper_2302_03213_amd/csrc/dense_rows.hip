@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void plain_pair_kernel(PlainArgs x, Plain
     __shared__ __align__(8) PlainShared shared;
     const int b = blockIdx.x;
     if (b >= x_blocks + w_blocks)
-        add_partial_sums<kThreads>(sums, b - x_blocks - w_blocks, &shared);
+        add_partial_sums<float, kThreads>(sums, b - x_blocks - w_blocks, &shared);
     else if (b < x_blocks)
         plain_f32_block<true, true>(x, b, shared);
     else

@@ -91,6 +91,19 @@ def test_large(lut, N, D, M, kind):
                     du.check(g, want, off)
 
 
+@pytest.mark.parametrize("kind", list(du.TYPES))
+@pytest.mark.parametrize("N", [1, 511, 2047, 2048, 2049])
+def test_bias_gradient_with_and_without_a_pass_of_its_own(lut, N, kind):
+    T = du.TYPES[kind]
+    for D, M, pad in ((24, 40, 8), (24, 40, 3), (520, 33, 0), (64, 1000, 24)):
+        X, W, _, _, G = operands(N, D, M, T, seed=N + D)
+        given = du.strided(G, pad, 8)
+        got = lut.dense_linear_backward(X, W, given)
+        for g, (want, off) in zip(got, du.dense_backward64(X, W, G, None, None)):
+            du.check(g, want, off)
+        assert torch.equal(got[2], lut.dense_linear_backward(X, W, given)[2])
+
+
 # fp32 of some hundred rows, and larger ones of odd widths: tiles that end early on either side and in k, widths around four
 MIDDLE = [(300, 65, 67), (1000, 100, 300), (257, 129, 5), (500, 5, 129), (700, 4, 4), (600, 3, 900), (600, 900, 3), (65, 1000, 1001),
           (2000, 33, 1), (90, 4100, 260), (2050, 1001, 1003), (4099, 1003, 1801)]
