@@ -5,8 +5,8 @@
 // The three products run on the matrix cores (dense_product.h), which want 16-bit operands whose rows are whole aligned 16-byte
 // vectors.  Matrices that are such go to them as they are; others are laid out in the workspace first: fp32 ones as three planes of
 // bf16 parts, 16-bit ones of odd widths, strides or addresses as copies with padded rows.  dZ is formed on the way there, and summed
-// for db in the same pass: 8192 x 4096 in bf16 with the slope of gelu_tanh 44 us, 4.6 TB/s.  fp32 products too small for that go
-// through the fp32 instructions as they are (dense_tile_f32.h, dense_rows.hip), and so do a few rows of any type (dense_rows.hip).
+// for db in the same pass: 8192 x 4096 in bf16 with the slope of gelu_tanh 44 us, 4.6 TB/s.  Products too small for that take
+// their operands as they are (dense_tile_as_is.h; dense_rows.hip: fp32 ones of up to a hundred rows, a few rows of any type).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -185,21 +185,27 @@ hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db
 struct TileSize {
     int i, j, depth, at_once;
     float stage[4], rest[4];
-    bool as_is = false;  // of fp32 operands that are not laid out
+    bool as_is = false;  // of operands that are not laid out
 };
 constexpr TileSize kTiles16[] = {{256, 256, 32, 1, {1.55f}, {9.0f}},
                                  {128, 128, 64, 2, {0.78f, 0.90f}, {2.0f, 5.0f}},
                                  {64, 128, 64, 2, {0.61f, 0.65f}, {0.5f, 2.5f}},
                                  {64, 64, 64, 3, {0.23f, 0.46f, 0.66f}, {1.0f, 0.7f, 1.0f}},
-                                 {32, 64, 64, 4, {0.16f, 0.37f, 0.56f, 0.72f}, {1.0f, 0.5f, 0.5f, 0.5f}}};
+                                 {32, 64, 64, 4, {0.16f, 0.37f, 0.56f, 0.72f}, {1.0f, 0.5f, 0.5f, 0.5f}},
+                                 {64, 64, 64, 2, {0.42f, 0.85f}, {1.4f, 1.8f}, true},
+                                 {32, 64, 64, 4, {0.37f, 0.60f, 0.75f, 1.10f}, {0.6f, 0.9f, 0.9f, 1.0f}, true}};
 constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.3f}, {8.4f}},
                                   {128, 128, 32, 1, {2.02f}, {3.7f}},
                                   {64, 64, 32, 2, {1.08f, 2.07f}, {1.5f, 1.7f}, true},
                                   {32, 32, 32, 2, {0.32f, 0.56f}, {0.8f, 0.8f}, true}};
 constexpr float kLaunchUs = 3.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
 
-// Laying `values` fp32 values out: read, and written as three parts, much of both in the caches.
-float lay_out_us(float values) { return 2.5f + values * 10 / 10e6f; }
+// Laying that many values out: fp32 ones read, and written as three parts, much of both in the caches; 16-bit ones from rows of any
+// alignment, none of them nothing.
+float lay_out_us(int dtype, float values) {
+    if (dtype == 0) return 2.5f + values * 10 / 10e6f;
+    return values > 0.f ? 2.7f + values * 4 / 2.6e6f : 0.f;
+}
 
 // A product's tile, how many of its tiles are one workgroup's, and how many workgroups share the sum of each of the others.
 struct Plan {
@@ -224,16 +230,16 @@ float tiles_us(const TileSize& t, float count, float stages, float units) {
 // lay_out: us for that.
 Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
-    const int count = dtype == 0 ? 4 : 5, units = compute_units();
-    const int64_t narrow = k_rows == 2 ? 4 : k_rows == 1 ? J : std::min<int64_t>(I, J);  // of operands that do not run along k
+    const int count = dtype == 0 ? 4 : 7, units = compute_units(), size = dtype == 0 ? 4 : 2;
+    const int64_t narrow = k_rows == 2 ? 8 : k_rows == 1 ? J : std::min<int64_t>(I, J);  // of operands that do not run along k
     Plan best = {0, 0, 1, 0, 1e30f, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
-        if (tiles > kMostTiles || (t.as_is && narrow < 4)) continue;
+        if (tiles > kMostTiles || (t.as_is && narrow < 16 / size)) continue;
         const float stage = t.depth / 64.f, launch = kLaunchUs + (t.as_is ? 0.f : lay_out);
         // what tiles that read their operands as they are have on its way: 2 us for two stages of every workgroup
-        const float bytes = t.as_is ? (float)(I + J) * K * 4 : 0.f, slots_bytes = (t.i + t.j) * t.depth * 4.f;
+        const float bytes = t.as_is ? (float)(I + J) * K * size : 0.f, slots_bytes = (float)((t.i + t.j) * t.depth * size);
         const auto memory_us = [&](float workgroups) { return bytes / (std::min(workgroups, (float)units * t.at_once) * slots_bytes); };
         const float us = launch + std::max(tiles_us(t, (float)tiles, k_tiles * stage, (float)units), memory_us((float)tiles));
         if (us < best.us) best = {i, (int)tiles, 1, tiles, us, t.as_is};
@@ -261,13 +267,13 @@ struct PairPlan {
 
 PairPlan pair_plan(int dtype, int64_t N, int D, int M, float lay_out) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
-    const int count = dtype == 0 ? 4 : 5;
+    const int count = dtype == 0 ? 4 : 7;
     const float units = (float)compute_units();
     PairPlan best = {0, 1, 1, 0, 0, 0, 1e30f, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t x_tiles = ((N + t.i - 1) / t.i) * ((D + t.j - 1) / t.j), w_tiles = ((int64_t)(D + t.i - 1) / t.i) * ((M + t.j - 1) / t.j);
-        if (std::max(x_tiles, w_tiles) > kMostTiles || (t.as_is && std::min(D, M) < 4)) continue;
+        if (std::max(x_tiles, w_tiles) > kMostTiles || (t.as_is && std::min(D, M) < (dtype == 0 ? 4 : 8))) continue;
         const float x_stages = (float)((M + t.depth - 1) / t.depth), w_stages = (float)((N + t.depth - 1) / t.depth);
         const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / kBytesPerUs;
         for (const int xs : {1, 2, 4}) {
@@ -354,7 +360,7 @@ Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t
 
 // What the backward pass has to have laid out, and its products: of both gradients in one launch, or of one.
 struct GradientPlan {
-    bool plain, as_is;  // fp32 products of the operands as they are: without tiles, or either way
+    bool plain, as_is;  // products of the operands as they are: fp32 ones without tiles, or either way
     bool x, w, z, sums, direct, pass, both;  // direct: db's sums are taken beside the products
     Plan one;
     PairPlan pair;
@@ -366,9 +372,11 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     GradientPlan g = {};
     g.both = need_dx && need_dw;
     float tiles = 0.f, plain = 0.f;
-    const float values = (float)c.N * c.M + (need_dx ? (float)c.D * c.M : 0.f) + (need_dw ? (float)c.N * c.D : 0.f);
+    const bool x_used = usable(c.dtype, c.X, c.ldx, c.D), w_used = usable(c.dtype, c.W, c.ldw, c.M), g_used = usable(c.dtype, G, ldg, c.M);
+    const float values = (g_used ? 0.f : (float)c.N * c.M) + (need_dx && !w_used ? (float)c.D * c.M : 0.f) +
+                         (need_dw && !x_used ? (float)c.N * c.D : 0.f);
     // the pass over G is there for an activation or a bias either way; planes are half as much again to write
-    const float lay_out = c.dtype == 0 ? lay_out_us(values) : 0.f;
+    const float lay_out = lay_out_us(c.dtype, values);
     if (g.both) {
         g.pair = pair_plan(c.dtype, c.N, c.D, c.M, lay_out);
         tiles = g.pair.us, plain = plain_pair_us(c.N, c.D, c.M), g.as_is = g.pair.as_is;
@@ -381,9 +389,9 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     }
     g.plain = c.dtype == 0 && plain < tiles;
     g.as_is |= g.plain;
-    g.x = !g.as_is && need_dw && !usable(c.dtype, c.X, c.ldx, c.D);
-    g.w = !g.as_is && need_dx && !usable(c.dtype, c.W, c.ldw, c.M);
-    g.z = (need_dx || need_dw) && (activation != 0 || (!g.as_is && !usable(c.dtype, G, ldg, c.M)));
+    g.x = !g.as_is && need_dw && !x_used;
+    g.w = !g.as_is && need_dx && !w_used;
+    g.z = (need_dx || need_dw) && (activation != 0 || (!g.as_is && !g_used));
     // Where nothing else has to read G before the products, few rows of it are added up beside them, 32 columns per workgroup, and
     // not in a pass of their own: 256 x 768 x 768 in bf16 8.0 us for 12.0, 2048 x 768 x 768 22.7 for 23.2, 4096 x 256 x 256 23.4 for 18.3.
     g.direct = need_db && g.both && !g.z && !g.x && !g.w && c.N <= kDirectRows;
@@ -400,7 +408,7 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
 }
 
 size_t slope_bytes(const DenseCall& c, const GradientPlan& g) {
-    return g.as_is ? (size_t)round_up(c.N * c.M * 4, 256) : laid_out_bytes(c.dtype, c.N, c.M);
+    return g.as_is && c.dtype == 0 ? (size_t)round_up(c.N * c.M * 4, 256) : laid_out_bytes(c.dtype, c.N, c.M);
 }
 size_t column_bytes(const GradientPlan& g, int M) { return g.sums ? (size_t)round_up((int64_t)g.slope.chunks * M * 4, 256) : 0; }
 
@@ -414,10 +422,11 @@ ForwardPlan forward_plan(const DenseCall& c) {
     ForwardPlan f = {};
     f.few = c.N <= kFewRows;
     if (f.few) return f;
-    f.product = plan(c.dtype, c.N, c.M, c.D, 1, c.dtype == 0 ? lay_out_us((float)c.N * c.D + (float)c.D * c.M) : 0.f);
+    const bool x_used = usable(c.dtype, c.X, c.ldx, c.D), w_used = usable(c.dtype, c.W, c.ldw, c.M);
+    f.product = plan(c.dtype, c.N, c.M, c.D, 1, lay_out_us(c.dtype, (x_used ? 0.f : (float)c.N * c.D) + (w_used ? 0.f : (float)c.D * c.M)));
     f.plain = c.dtype == 0 && plain_f32_us(c.N, c.M, c.D) < f.product.us;
-    f.x = !f.plain && !f.product.as_is && !usable(c.dtype, c.X, c.ldx, c.D);
-    f.w = !f.plain && !f.product.as_is && !usable(c.dtype, c.W, c.ldw, c.M);
+    f.x = !f.plain && !f.product.as_is && !x_used;
+    f.w = !f.plain && !f.product.as_is && !w_used;
     return f;
 }
 
@@ -472,7 +481,7 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     if (g.pass) {
         SlopeArgs& a = g.slope;
         a.G = G, a.Z = Z, a.ldg = ldg, a.ldz = ldz, a.N = c.N, a.M = c.M, a.activation = activation;
-        a.to = z, a.plain = g.as_is, a.partial = g.sums ? columns : nullptr;
+        a.to = z, a.plain = g.as_is && c.dtype == 0, a.partial = g.sums ? columns : nullptr;
         const hipError_t e = with_type(c.dtype, [&](auto t) {
             hipLaunchKernelGGL(slope_kernel<decltype(t)>, dim3((unsigned)(a.chunks * a.col_tiles) + lay_out_blocks(others)), dim3(256), 0, s,
                                a, others);
@@ -497,7 +506,7 @@ hipError_t launch_dense_linear_gradient(const DenseCall& c, const void* G, int64
     }
     const bool f32 = c.dtype == 0;
     const auto gradient = [&](bool k_inner) {
-        if (g.as_is && z) return operand(z, c.M, nullptr, c.N, c.M, k_inner, f32);
+        if (g.as_is && z && f32) return operand(z, c.M, nullptr, c.N, c.M, k_inner, f32);
         Operand o = operand(G, ldg, z, c.N, c.M, k_inner, f32);
         if (f32 && activation) {
             o.slope_of = static_cast<const float*>(Z), o.activation = activation;

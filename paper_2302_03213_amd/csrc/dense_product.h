@@ -14,13 +14,13 @@
 //   - The next step's operands are read from LDS while a step's products run, a read between every two.
 //   - Operands whose rows do not run along k are turned by the LDS reads, so that no layout needs a pass over memory.
 //   - XORed units keep those reads from meeting in a bank.  Tiles go to the XCDs in contiguous ranges, four rows of tiles at a time.
-// Operands of odd strides or addresses are laid out first: loads of them through registers took 1.4 times as long as that and the
-// product.  Which tile, and whether a sum is shared out: dense_linear.hip.
+// Operands of odd strides or addresses are laid out first, or go through dense_tile_as_is.h.  Which tile, and whether a sum is shared
+// out: dense_linear.hip.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "dense_tile_f32.h"
+#include "dense_tile_as_is.h"
 #include "lutnn_kernels.h"
 #include "mfma_tile.h"
 #include "split_bf16.h"
@@ -29,18 +29,8 @@ namespace lutnn {
 namespace product {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kBeyond = 0xc0000000u;  // an offset past any tile's rows: the load gives zeros
-
-__device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, bf16) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
 
 // What a wavefront's lanes have written to LDS is there for its other lanes.
 __device__ __forceinline__ void wave_sync() {
@@ -430,7 +420,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, int block, ch
 template <class C, bool A_K, bool B_K>
 __device__ __forceinline__ void any_tile(const ProductArgs& a, int block, char* const lds) {
     if constexpr (C::AS_IS)
-        tile_f32<C, A_K, B_K>(a, block, lds);
+        tile_as_is<C, A_K, B_K>(a, block, lds);
     else
         product_tile<C, A_K, B_K>(a, block, lds);
 }
@@ -539,8 +529,8 @@ hipError_t with_tile(int tile, F&& f) {
         switch (tile) {
             case 0: return f(Config<T, 128, 256, 2, 4, 32, 2>());
             case 1: return f(Config<T, 128, 128, 2, 4, 32, 2>());
-            case 2: return f(ConfigF32<64, 64, 2, 4, 32, 4>());
-            default: return f(ConfigF32<32, 32, 2, 2, 32, 4>());
+            case 2: return f(ConfigAsIs<T, 64, 64, 2, 4, 32, 4>());
+            default: return f(ConfigAsIs<T, 32, 32, 2, 2, 32, 4>());
         }
     } else {
         switch (tile) {
@@ -548,7 +538,9 @@ hipError_t with_tile(int tile, F&& f) {
             case 1: return f(Config<T, 128, 128, 2, 4, 64, 2>());
             case 2: return f(Config<T, 64, 128, 2, 4, 64, 2>());
             case 3: return f(Config<T, 64, 64, 2, 2, 64, 3>());
-            default: return f(Config<T, 32, 64, 1, 4, 64, 3>());
+            case 4: return f(Config<T, 32, 64, 1, 4, 64, 3>());
+            case 5: return f(ConfigAsIs<T, 64, 64, 2, 2, 64, 2>());
+            default: return f(ConfigAsIs<T, 32, 64, 1, 4, 64, 2>());
         }
     }
 }

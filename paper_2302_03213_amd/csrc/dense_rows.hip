@@ -103,7 +103,7 @@ __device__ __forceinline__ void load_fragment(const PlainOperand& o, int64_t fir
 // 16 rows by 16 columns per workgroup on the fp32 matrix instructions, straight from memory: the wavefronts take every eighth 16 k,
 // two of them ahead, and add up in LDS.  An instruction sums four k, one per 16 lanes: lane group q holds k = 4 q .. 4 q + 3 of both
 // operands, and instruction r takes the r-th of each.  Blocks: row blocks * column blocks, row block fastest.  What bounds it is
-// latency: 37 x 768 x 768 5.6 us, where the tiles of dense_tile_f32.h take 7.4; from 128 rows on those are as fast.
+// latency: 37 x 768 x 768 5.6 us, where the tiles of dense_tile_as_is.h take 7.4; from 128 rows on those are as fast.
 struct PlainArgs {
     PlainOperand A, B;
     int64_t I, K;

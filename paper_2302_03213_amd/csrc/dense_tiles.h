@@ -6,6 +6,9 @@
 
 #include "dense_epilogue.h"
 #include "dense_rows.h"
+#include "matrix_types.h"
+#include "mfma_tile.h"
+#include "split_bf16.h"
 
 namespace lutnn {
 
@@ -42,6 +45,17 @@ struct PairArgs {
 namespace product {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// 32 k of 16 rows and columns, eight per lane.
+__device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, bf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c, f16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 
 // Orders the workgroup's LDS operations only: loads to LDS stay in flight.
 __device__ __forceinline__ void lds_barrier() {

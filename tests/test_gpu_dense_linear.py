@@ -104,15 +104,16 @@ def test_bias_gradient_with_and_without_a_pass_of_its_own(lut, N, kind):
         assert torch.equal(got[2], lut.dense_linear_backward(X, W, given)[2])
 
 
-# fp32 of some hundred rows, and larger ones of odd widths: tiles that end early on either side and in k, widths around four
+# some hundred rows, and more of odd widths: tiles that end early on either side and in k, widths around a load's four or eight values
 MIDDLE = [(300, 65, 67), (1000, 100, 300), (257, 129, 5), (500, 5, 129), (700, 4, 4), (600, 3, 900), (600, 900, 3), (65, 1000, 1001),
-          (2000, 33, 1), (90, 4100, 260), (2050, 1001, 1003), (4099, 1003, 1801)]
+          (2000, 33, 1), (90, 4100, 260), (2050, 1001, 1003), (4099, 1003, 1801), (200, 9, 15), (300, 7, 500), (300, 500, 7), (513, 127, 8)]
 
 
+@pytest.mark.parametrize("kind", list(du.TYPES))
 @pytest.mark.parametrize("pad", [0, 1])
 @pytest.mark.parametrize("N,D,M", MIDDLE)
-def test_middle_sizes_in_fp32(lut, N, D, M, pad):
-    X, W, b, R, G = operands(N, D, M, torch.float32, seed=N + D + M)
+def test_middle_sizes(lut, N, D, M, pad, kind):
+    X, W, b, R, G = operands(N, D, M, du.TYPES[kind], seed=N + D + M)
     if pad:
         X, W, R, G = (du.strided(t, pad, 1) for t in (X, W, R, G))
     Y = lut.dense_linear(X, W, b, "gelu", R)
