@@ -141,17 +141,43 @@ struct NormGradientArgs {
     T* dX;
     float* partial;  // [workgroups][2][D]
     int64_t N, ldg, ldx, ldr, lddx;
-    int D;
+    int D, row_blocks;
+    float *dw, *db;  // of the workgroups behind row_blocks
 };
+
+// dw and db of THREADS / 16 columns, every row of them read again, by 16 groups of threads.  part: two per thread.
+template <class T, int THREADS>
+__device__ __forceinline__ void sum_columns(const NormGradientArgs<T>& a, int block, float* part) {
+    constexpr int GROUPS = 16, COLUMNS = THREADS / GROUPS;
+    const int group = threadIdx.x / COLUMNS, d = block * COLUMNS + threadIdx.x % COLUMNS, at = min(d, a.D - 1);
+    float sums[2] = {0.f, 0.f};
+#pragma unroll 8
+    for (int64_t n = group; n < a.N; n += GROUPS) {
+        const float g = (float)a.G[n * a.ldg + at], x = (float)a.X[n * a.ldx + at];
+        sums[0] = __fmaf_rn(g, (x - a.statistics[2 * n]) * a.statistics[2 * n + 1], sums[0]);
+        sums[1] += g;
+    }
+    part[2 * threadIdx.x] = sums[0];
+    part[2 * threadIdx.x + 1] = sums[1];
+    __syncthreads();
+    if (group != 0 || d >= a.D) return;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) sums[v] += part[2 * (threadIdx.x + i * COLUMNS) + v];
+    if (a.dw) a.dw[d] = sums[0];
+    if (a.db) a.db[d] = sums[1];
+}
 
 // Rows are dealt to the workgroups in turn; each keeps the column sums of its own in registers and leaves them in `partial`.  The fewer
 // workgroups, the fewer sums are left, so that the next row's loads have to hide the memory's latency: 16384 x 4096 in bf16 with a
-// residual 107 us, 537 MB at the rate of a large copy; 168 without them.
-template <class T, int VEC, int TPR>
+// residual 107 us, 537 MB at the rate of a large copy; 168 without them.  SUMS: whether any are kept.
+template <class T, int VEC, int TPR, bool SUMS>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gradient_kernel(NormGradientArgs<T> a) {
     constexpr int THREADS = TPR < kThreads ? kThreads : TPR, ROWS = THREADS / TPR, CH = VEC == 1 ? 1 : kValues / VEC;
     __shared__ float shared[4 * (TPR > 64 ? TPR / 64 : 1)];
-    __shared__ float parts[2][ROWS > 1 ? CH * VEC : 1][THREADS];
+    __shared__ float parts[2][SUMS && ROWS > 1 ? CH * VEC : 1][THREADS];
+    if (!SUMS && (int)blockIdx.x >= a.row_blocks) return sum_columns<T, THREADS>(a, blockIdx.x - a.row_blocks, &parts[0][0][0]);
     int turn = 0;
     const Columns<VEC, TPR> col{a.D, (int)(threadIdx.x % TPR)};
     float dw[CH][VEC] = {}, db[CH][VEC] = {}, w[CH][VEC];
@@ -191,7 +217,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
         else
             return (float)v[j];
     };
-    const int64_t first = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR, step = (int64_t)gridDim.x * ROWS;
+    const int64_t first = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR, step = (int64_t)a.row_blocks * ROWS;
     Row next;
     if constexpr (AHEAD) {
         load_weight();
@@ -212,7 +238,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
             for (int j = 0; j < VEC; ++j) {
                 g[c][j] = value(row.g[c], j);
                 h[c][j] = (value(row.x[c], j) - row.mean) * row.rstd;
-                if (col.mine(c, j)) {
+                if (SUMS && col.mine(c, j)) {
                     dw[c][j] = __fmaf_rn(g[c][j], h[c][j], dw[c][j]);
                     db[c][j] += g[c][j];
                 }
@@ -221,7 +247,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
                 sums[1] += col.mine(c, j) ? g[c][j] * h[c][j] : 0.f;
             }
         }
-        if (!a.dX) continue;
+        if (SUMS && !a.dX) continue;
         row_sums<TPR>(sums, shared, turn);
         const float q = sums[0] / a.D, qh = sums[1] / a.D;
 #pragma unroll
@@ -235,7 +261,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void layer_norm_gr
             store_values(a.dX + n * a.lddx + col.at(c), g[c]);
         }
     }
-    if (!a.partial) return;
+    if constexpr (!SUMS) return;
     float* const mine = a.partial + (int64_t)blockIdx.x * 2 * a.D;
     if constexpr (ROWS > 1) {  // the workgroup's rows, in order, a column per thread and turn
 #pragma unroll
@@ -285,6 +311,11 @@ hipError_t by_width(int D, F&& f) {
 
 int rows_per_workgroup(int D) { return D <= 16 * kValues ? kThreads / 16 : D <= 64 * kValues ? kThreads / 64 : 1; }
 
+// Few rows are read again for dw and db beside dX, and not summed by workgroup and then over those: 256 x 768 6.0 us for 9.8,
+// 256 x 4096 in fp32 6 for 13 (bf16 6 for 15), 1024 x 4096 22 for 20 (14 for 26), 1024 x 16384 67 for 94 (33 for 56), 1536 x 4096 32 for
+// 23 (21 for 25).
+constexpr int64_t kDirectRows = 1024;
+
 // Two workgroups per compute unit, one for rows of more than four wavefronts.  4096 x 768 in fp32: 9.2 us (one: 9.6, four: 11.0); 16384 x 4096 in
 // bf16 82 (one: 101, three: 90), with a residual 107 (one: 104, three: 112).
 int gradient_workgroups(int64_t N, int D) {
@@ -295,7 +326,9 @@ int gradient_workgroups(int64_t N, int D) {
 
 }  // namespace
 
-size_t layer_norm_gradient_workspace(int64_t N, int D) { return (size_t)gradient_workgroups(N, D) * 2 * D * sizeof(float); }
+size_t layer_norm_gradient_workspace(int64_t N, int D) {
+    return N <= kDirectRows ? 0 : (size_t)gradient_workgroups(N, D) * 2 * D * sizeof(float);
+}
 
 hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
                              const float* b, float eps, void* Y, int64_t ldy, void* S, int64_t lds, float* statistics,
@@ -316,24 +349,29 @@ hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, i
 hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
                                       const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
                                       float* dw, float* db, void* workspace, hipStream_t s) {
-    float* const partial = dw || db ? static_cast<float*>(workspace) : nullptr;
-    const int groups = gradient_workgroups(N, D);
+    const bool direct = N <= kDirectRows && (dw || db);
+    float* const partial = !direct && (dw || db) ? static_cast<float*>(workspace) : nullptr;
+    const int groups = gradient_workgroups(N, D), rows = dX || partial ? groups : 0;
     if (groups > 0) {
         const hipError_t e = with_type(dtype, [&](auto t) {
             using T = decltype(t);
             const NormGradientArgs<T> a{static_cast<const T*>(G), static_cast<const T*>(X), static_cast<const T*>(R), statistics, w,
-                                        static_cast<T*>(dX), partial, N, ldg, ldx, ldr, lddx, D};
+                                        static_cast<T*>(dX), partial, N, ldg, ldx, ldr, lddx, D, rows, dw, db};
             return by_width<T>(D, [&](auto vec, auto tpr) {
                 constexpr int TPR = decltype(tpr)::value;
-                hipLaunchKernelGGL((layer_norm_gradient_kernel<T, decltype(vec)::value, TPR>), dim3((unsigned)groups),
-                                   dim3(TPR < kThreads ? kThreads : TPR), 0, s, a);
+                constexpr int THREADS = TPR < kThreads ? kThreads : TPR, COLUMNS = THREADS / 16;
+                const dim3 grid((unsigned)(rows + (direct ? (D + COLUMNS - 1) / COLUMNS : 0))), threads(THREADS);
+                if (partial)
+                    hipLaunchKernelGGL((layer_norm_gradient_kernel<T, decltype(vec)::value, TPR, true>), grid, threads, 0, s, a);
+                else
+                    hipLaunchKernelGGL((layer_norm_gradient_kernel<T, decltype(vec)::value, TPR, false>), grid, threads, 0, s, a);
                 return hipGetLastError();
             });
         });
         if (e != hipSuccess) return e;
     }
-    if (!dw && !db) return hipSuccess;
-    return launch_partial_sums(static_cast<const float*>(workspace), groups, 2 * D, D, dw, db, s);
+    if ((!dw && !db) || (direct && N > 0)) return hipSuccess;
+    return launch_partial_sums(partial, groups, 2 * D, D, dw, db, s);
 }
 
 }  // namespace lutnn

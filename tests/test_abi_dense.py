@@ -106,11 +106,12 @@ def test_layer_norm_refusals(lut):
 
 def test_layer_norm_backward_refusals(lut):
     call = norm_backward(lut)
-    for name in ("G", "X", "statistics", "workspace"):
+    for name in ("G", "X", "statistics"):
         assert call.refused(**{name: None}) == "LUTNN_E_NULL", name
     assert call.refused(D=16385) == "LUTNN_E_UNSUPPORTED"
-    assert call.refused(workspace=0x90004) == "LUTNN_E_ALIGN"
-    assert call.refused(bytes=0) == "LUTNN_E_SHAPE"
+    assert call.refused(N=1025, workspace=None) == "LUTNN_E_NULL"  # fewer rows of that width need none
+    assert call.refused(N=1025, workspace=0x90004) == "LUTNN_E_ALIGN"
+    assert call.refused(N=1025, bytes=0) == "LUTNN_E_SHAPE"
 
 
 def test_workspace_queries(lut):
