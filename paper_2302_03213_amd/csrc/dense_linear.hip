@@ -420,7 +420,7 @@ struct ForwardPlan {
 
 ForwardPlan forward_plan(const DenseCall& c) {
     ForwardPlan f = {};
-    f.few = c.N <= kFewRows;
+    f.few = few_rows(c.dtype, c.N, c.D, c.M);
     if (f.few) return f;
     const bool x_used = usable(c.dtype, c.X, c.ldx, c.D), w_used = usable(c.dtype, c.W, c.ldw, c.M);
     f.product = plan(c.dtype, c.N, c.M, c.D, 1, lay_out_us(c.dtype, (x_used ? 0.f : (float)c.N * c.D) + (w_used ? 0.f : (float)c.D * c.M)));

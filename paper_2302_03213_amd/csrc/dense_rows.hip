@@ -11,7 +11,6 @@ namespace lutnn {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64;
-constexpr int kCols = 16;  // of a workgroup
 
 // Workgroup b's strip of columns: contiguous ranges on each XCD, as the strips of one 128-byte line of W share its L2.
 __device__ __forceinline__ int strip_of(int b, int strips) {
@@ -19,18 +18,18 @@ __device__ __forceinline__ int strip_of(int b, int strips) {
     return t < strips ? t : -1;
 }
 
-// A strip of 16 columns per workgroup.  A lane reads 16 bytes of a row of W, 2 (fp32: 4) lanes a row, and a workgroup 256 (128) rows
-// at a time, AHEAD times that in flight; the sums over k stay in the lane to the end, and go through the wavefront and LDS then.
-// grid: strips.
-template <class T, int ROWS>
+// A strip of COLS columns per workgroup.  A lane reads 16 bytes of a row of W, 2 (fp32: 4) lanes a row of 16 columns, and a workgroup
+// 256 (128) such rows at a time, AHEAD times that in flight; the sums over k stay in the lane to the end, and go through the
+// wavefront and LDS then.  grid: strips.
+template <class T, int ROWS, int COLS>
 __global__ __launch_bounds__(kThreads) void few_rows_kernel(const T* __restrict__ X, int N, int64_t ldx, const T* __restrict__ W,
                                                             int64_t ldw, int D, int M, int strips, Epilogue e) {
-    constexpr int V = 16 / sizeof(T), LANES = kCols / V, STEP = kThreads / LANES, AHEAD = 4;
-    __shared__ float part[kWaves][ROWS][kCols];
+    constexpr int V = 16 / sizeof(T), LANES = COLS / V, STEP = kThreads / LANES, AHEAD = 4;
+    __shared__ float part[kWaves][ROWS][COLS];
     const int strip = strip_of(blockIdx.x, strips);
     if (strip < 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int j = strip * kCols + lane % LANES * V;
+    const int j = strip * COLS + lane % LANES * V;
     const bool whole = j + V <= M;
     float sum[ROWS][V] = {};
     const auto add = [&](auto count, int k0) {
@@ -71,7 +70,7 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(const T* __restrict_
 #pragma unroll
             for (int c = 0; c < V; ++c) part[wave][r][lane * V + c] = sum[r][c];
     __syncthreads();
-    const int r = threadIdx.x / kCols, c = threadIdx.x % kCols, col = strip * kCols + c;
+    const int r = threadIdx.x / COLS, c = threadIdx.x % COLS, col = strip * COLS + c;
     if (r >= N || r >= ROWS || col >= M) return;
     float z[1][1] = {{0.f}}, bias[1];
 #pragma unroll
@@ -204,16 +203,31 @@ constexpr float kLaunchUs = 2.6f, kPerK = 0.0033f, kRest = 0.27f;
 
 hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int D, int M,
                            const Epilogue& e, hipStream_t s) {
-    const int strips = (M + kCols - 1) / kCols;
+    // Wider strips read W in longer pieces, where there are enough of them: 1 x 8192 x 8192 in fp32 48 us by 16 columns, 41 by 32, 38 by
+    // 64; 4096 wide 14, 13 and 19; in bf16 1 x 4096 x 11008 25, 21 and 32, 4096 wide 12, 16 and 29.
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        const auto launch = [&](auto rows) {
-            hipLaunchKernelGGL((few_rows_kernel<T, decltype(rows)::value>), dim3((unsigned)(strips + 7) / 8 * 8), dim3(kThreads), 0, s,
+        using std::integral_constant;
+        constexpr int kEnough = 512 / sizeof(T);
+        const auto launch = [&](auto rows, auto cols) {
+            constexpr int ROWS = decltype(rows)::value, COLS = decltype(cols)::value;
+            const int strips = (M + COLS - 1) / COLS;
+            hipLaunchKernelGGL((few_rows_kernel<T, ROWS, COLS>), dim3((unsigned)(strips + 7) / 8 * 8), dim3(kThreads), 0, s,
                                static_cast<const T*>(X), (int)N, ldx, static_cast<const T*>(W), ldw, D, M, strips, e);
             return hipGetLastError();
         };
-        if (N == 1) return launch(std::integral_constant<int, 1>());
-        return N == 2 ? launch(std::integral_constant<int, 2>()) : launch(std::integral_constant<int, kFewRows>());
+        const auto by_width = [&](auto rows) {
+            if constexpr (sizeof(T) == 4)
+                if (M / 64 >= kEnough) return launch(rows, integral_constant<int, 64>());
+            if (M / 32 >= kEnough) return launch(rows, integral_constant<int, 32>());
+            return launch(rows, integral_constant<int, 16>());
+        };
+        if (N == 1) return by_width(integral_constant<int, 1>());
+        if constexpr (sizeof(T) == 4) {
+            if (N > 4) return by_width(integral_constant<int, 8>());
+            if (N > 2) return by_width(integral_constant<int, 4>());
+        }
+        return by_width(integral_constant<int, 2>());
     });
 }
 

@@ -104,6 +104,18 @@ def test_bias_gradient_with_and_without_a_pass_of_its_own(lut, N, kind):
         assert torch.equal(got[2], lut.dense_linear_backward(X, W, given)[2])
 
 
+@pytest.mark.parametrize("kind", list(du.TYPES))
+@pytest.mark.parametrize("N", [1, 2, 3, 4, 5, 7, 8, 9])
+def test_few_rows(lut, N, kind):
+    """Of small and of large W, of widths that are whole strips of columns and that are not."""
+    for D, M, pad in ((130, 4096, 0), (2050, 4100, 3), (1024, 8192, 8), (1030, 8203, 1), (300, 17, 0)):
+        X, W, b, R, _ = operands(N, D, M, du.TYPES[kind], seed=N + D)
+        if pad:
+            X, W, R = (du.strided(t, pad) for t in (X, W, R))
+        Y = lut.dense_linear(X, W, b, "silu", R)
+        du.check(Y, *du.dense64(X, W, b, "silu", R)[:2])
+
+
 # some hundred rows, and more of odd widths: tiles that end early on either side and in k, widths around a load's four or eight values
 MIDDLE = [(300, 65, 67), (1000, 100, 300), (257, 129, 5), (500, 5, 129), (700, 4, 4), (600, 3, 900), (600, 900, 3), (65, 1000, 1001),
           (2000, 33, 1), (90, 4100, 260), (2050, 1001, 1003), (4099, 1003, 1801), (200, 9, 15), (300, 7, 500), (300, 500, 7), (513, 127, 8)]
