@@ -204,11 +204,13 @@ constexpr float kLaunchUs = 2.6f, kPerK = 0.0033f, kRest = 0.27f;
 hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int D, int M,
                            const Epilogue& e, hipStream_t s) {
     // Wider strips read W in longer pieces, where there are enough of them: 1 x 8192 x 8192 in fp32 48 us by 16 columns, 41 by 32, 38 by
-    // 64; 4096 wide 14, 13 and 19; in bf16 1 x 4096 x 11008 25, 21 and 32, 4096 wide 12, 16 and 29.
+    // 64; 4096 wide 14, 13 and 19; in bf16 1 x 4096 x 11008 25, 21 and 32, 4096 wide 12, 16 and 29.  Long sums of few columns go by
+    // strips of one load: 1 x 4096 x 1024 in fp32 10.5 us by 16 columns, 8.7 by four, in bf16 10.0 and 8.3 by eight; 1 x 768 x 768 3.9
+    // and 3.9, in bf16 4.0 and 4.6.
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         using std::integral_constant;
-        constexpr int kEnough = 512 / sizeof(T);
+        constexpr int kEnough = 512 / sizeof(T), kLoad = 16 / sizeof(T);
         const auto launch = [&](auto rows, auto cols) {
             constexpr int ROWS = decltype(rows)::value, COLS = decltype(cols)::value;
             const int strips = (M + COLS - 1) / COLS;
@@ -217,6 +219,7 @@ hipError_t launch_few_rows(int dtype, const void* X, int64_t N, int64_t ldx, con
             return hipGetLastError();
         };
         const auto by_width = [&](auto rows) {
+            if (D >= 2048 && M <= 256 * kLoad) return launch(rows, integral_constant<int, kLoad>());
             if constexpr (sizeof(T) == 4)
                 if (M / 64 >= kEnough) return launch(rows, integral_constant<int, 64>());
             if (M / 32 >= kEnough) return launch(rows, integral_constant<int, 32>());

@@ -108,7 +108,7 @@ def test_bias_gradient_with_and_without_a_pass_of_its_own(lut, N, kind):
 @pytest.mark.parametrize("N", [1, 2, 3, 4, 5, 7, 8, 9])
 def test_few_rows(lut, N, kind):
     """Of small and of large W, of widths that are whole strips of columns and that are not."""
-    for D, M, pad in ((130, 4096, 0), (2050, 4100, 3), (1024, 8192, 8), (1030, 8203, 1), (300, 17, 0)):
+    for D, M, pad in ((130, 4096, 0), (2050, 4100, 3), (1024, 8192, 8), (1030, 8203, 1), (300, 17, 0), (4097, 1021, 2), (2048, 40, 0)):
         X, W, b, R, _ = operands(N, D, M, du.TYPES[kind], seed=N + D)
         if pad:
             X, W, R = (du.strided(t, pad) for t in (X, W, R))
