@@ -198,7 +198,15 @@ constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.3f}, {8.4f}},
                                   {128, 128, 32, 1, {2.02f}, {3.7f}},
                                   {64, 64, 32, 2, {1.08f, 2.07f}, {1.5f, 1.7f}, true},
                                   {32, 32, 32, 2, {0.32f, 0.56f}, {0.8f, 0.8f}, true}};
-constexpr float kLaunchUs = 3.5f, kJoinUs = 5.f, kBytesPerUs = 3.5e6f;
+constexpr float kLaunchUs = 3.5f;
+
+// What sharing a sum out costs beside the shares: the second launch, and the shares written and read again, which of one 16-bit product
+// are in the caches more often.  64 x 4096 x 4096 in bf16 13.3 us by four, 17.1 by tiles of half the rows; both gradients' products
+// chosen so took up to 14 % longer.
+struct Join {
+    float us, bytes_per_us;
+};
+constexpr Join kJoin = {5.f, 3.5e6f}, kJoin16 = {3.5f, 5e6f};
 
 // Laying that many values out: fp32 ones read, and written as three parts, much of both in the caches; 16-bit ones from rows of any
 // alignment, none of them nothing.
@@ -232,6 +240,7 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 7, units = compute_units(), size = dtype == 0 ? 4 : 2;
     const int64_t narrow = k_rows == 2 ? 8 : k_rows == 1 ? J : std::min<int64_t>(I, J);  // of operands that do not run along k
+    const Join join = dtype == 0 ? kJoin : kJoin16;
     Plan best = {0, 0, 1, 0, 1e30f, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
@@ -244,10 +253,10 @@ Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
         const float us = launch + std::max(tiles_us(t, (float)tiles, k_tiles * stage, (float)units), memory_us((float)tiles));
         if (us < best.us) best = {i, (int)tiles, 1, tiles, us, t.as_is};
         const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
-        const float base = launch + kJoinUs + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
+        const float base = launch + join.us + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
         if (shared == 0) continue;
         for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / kBytesPerUs;
+            const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / join.bytes_per_us;
             if (splits > k_tiles || moved >= best.us || shared * splits > kMostTiles) break;
             const float shared_us = moved + std::max(tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units),
                                                      memory_us((float)tiles + (float)shared * (splits - 1)));
@@ -269,13 +278,14 @@ PairPlan pair_plan(int dtype, int64_t N, int D, int M, float lay_out) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 7;
     const float units = (float)compute_units();
+    const Join join = kJoin;
     PairPlan best = {0, 1, 1, 0, 0, 0, 1e30f, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t x_tiles = ((N + t.i - 1) / t.i) * ((D + t.j - 1) / t.j), w_tiles = ((int64_t)(D + t.i - 1) / t.i) * ((M + t.j - 1) / t.j);
         if (std::max(x_tiles, w_tiles) > kMostTiles || (t.as_is && std::min(D, M) < (dtype == 0 ? 4 : 8))) continue;
         const float x_stages = (float)((M + t.depth - 1) / t.depth), w_stages = (float)((N + t.depth - 1) / t.depth);
-        const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / kBytesPerUs;
+        const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / join.bytes_per_us;
         for (const int xs : {1, 2, 4}) {
             if (xs > 1 && (xs > x_stages || x_tiles > slots)) break;
             for (const int ws : {1, 2, 4, 8, 16, 32}) {
@@ -287,7 +297,7 @@ PairPlan pair_plan(int dtype, int64_t N, int D, int M, float lay_out) {
                 const float x = kx * t.stage[at_once] + t.rest[at_once], w = kw * t.stage[at_once] + t.rest[at_once];
                 float us = std::max(x, w);
                 if (nx + nw > slots) us = std::max(us, (nx * x + nw * w) / slots + 0.4f * std::max(x, w));
-                us += kLaunchUs + (t.as_is ? 0.f : lay_out) + (xs > 1 ? kJoinUs + nx * tile_bytes : 0.f) + (ws > 1 ? kJoinUs + nw * tile_bytes : 0.f);
+                us += kLaunchUs + (t.as_is ? 0.f : lay_out) + (xs > 1 ? join.us + nx * tile_bytes : 0.f) + (ws > 1 ? join.us + nw * tile_bytes : 0.f);
                 if (us < best.us) best = {i, xs, ws, x >= w, x_tiles, w_tiles, us, t.as_is};
             }
         }
