@@ -316,10 +316,11 @@ int rows_per_workgroup(int D) { return D <= 16 * kValues ? kThreads / 16 : D <= 
 // 23 (21 for 25).
 constexpr int64_t kDirectRows = 1024;
 
-// Two workgroups per compute unit, one for rows of more than four wavefronts.  4096 x 768 in fp32: 9.2 us (one: 9.6, four: 11.0); 16384 x 4096 in
-// bf16 82 (one: 101, three: 90), with a residual 107 (one: 104, three: 112).
-int gradient_workgroups(int64_t N, int D) {
-    const int64_t most = (D <= 256 * kValues ? 2 : 1) * (int64_t)compute_units();
+// Two workgroups per compute unit; one for rows of more than four wavefronts, and where a row's loads keep the memory busy and sums
+// are left: 4096 x 768 in fp32 9.2 us (one: 9.6, four: 11.0), 16384 x 4096 in bf16 86 (one: 107), with a residual, 24 KB a row, 111
+// (one: 109, 2048 rows 27.7 and 24.8), in fp32 with one, 48 KB, 211 (one: 199).
+int gradient_workgroups(int64_t N, int D, int64_t row_bytes = 0) {
+    const int64_t most = (D <= 256 * kValues && row_bytes < 24 << 10 ? 2 : 1) * (int64_t)compute_units();
     const int rows = rows_per_workgroup(D);
     return (int)std::min<int64_t>((N + rows - 1) / rows, most);
 }
@@ -351,7 +352,8 @@ hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64
                                       float* dw, float* db, void* workspace, hipStream_t s) {
     const bool direct = N <= kDirectRows && (dw || db);
     float* const partial = !direct && (dw || db) ? static_cast<float*>(workspace) : nullptr;
-    const int groups = gradient_workgroups(N, D), rows = dX || partial ? groups : 0;
+    const int64_t row_bytes = partial ? (int64_t)D * (dtype == 0 ? 4 : 2) * (R && dX ? 3 : 2) : 0;
+    const int groups = gradient_workgroups(N, D, row_bytes), rows = dX || partial ? groups : 0;
     if (groups > 0) {
         const hipError_t e = with_type(dtype, [&](auto t) {
             using T = decltype(t);
