@@ -316,11 +316,13 @@ int rows_per_workgroup(int D) { return D <= 16 * kValues ? kThreads / 16 : D <= 
 // 23 (21 for 25).
 constexpr int64_t kDirectRows = 1024;
 
-// Two workgroups per compute unit; one for rows of more than four wavefronts, and where a row's loads keep the memory busy and sums
-// are left: 4096 x 768 in fp32 9.2 us (one: 9.6, four: 11.0), 16384 x 4096 in bf16 86 (one: 107), with a residual, 24 KB a row, 111
-// (one: 109, 2048 rows 27.7 and 24.8), in fp32 with one, 48 KB, 211 (one: 199).
+// Two workgroups per compute unit; one for rows of more than four wavefronts, and, where sums are left (row_bytes: what a row reads
+// then), for rows whose loads keep the memory busy and for few rows beside wide sums: 4096 x 768 in fp32 9.2 us (one: 9.6, four: 11.0),
+// 16384 x 4096 in bf16 86 (one: 107), with a residual, 24 KB a row, 111 (one: 109), in fp32 with one, 48 KB, 211 (one: 199); 2048 x 3000
+// in bf16 23.4 (one: 22.2), 1536 x 4096 25.3 (one: 21.3), 3080 x 4096 29.9 (one: 30.7).
 int gradient_workgroups(int64_t N, int D, int64_t row_bytes = 0) {
-    const int64_t most = (D <= 256 * kValues && row_bytes < 24 << 10 ? 2 : 1) * (int64_t)compute_units();
+    const bool one = D > 256 * kValues || row_bytes >= 24 << 10 || (row_bytes > 0 && N <= 2048 && D > 2048);
+    const int64_t most = (one ? 1 : 2) * (int64_t)compute_units();
     const int rows = rows_per_workgroup(D);
     return (int)std::min<int64_t>((N + rows - 1) / rows, most);
 }
