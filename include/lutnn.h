@@ -506,8 +506,9 @@ LUTNN_API size_t lutnn_dense_linear_workspace_bytes(int32_t dtype, const void* X
 
 /*
  * Its gradients from G = dL/dY:  dZ = G * activation'(Z),  dX = dZ . W^T,  dW = X^T . dZ,  dbias = the sum of dZ over its rows.
- * The residual's gradient is G itself.  dZ is rounded to `dtype` before it is multiplied, as the operands of the products are;
- * dbias is summed from what was not rounded.
+ * The residual's gradient is G itself.  dZ is rounded to `dtype` before it is multiplied, as the operands of the products are (in
+ * fp16 it is infinite there beyond 65504, as an output would be); dbias is summed from what was not rounded.  Without an activation
+ * and with RELU that changes nothing; with the others the rounding of dX and dW in 16 bits weighs sqrt 2 times what it does alone.
  *
  *   G [N][M]; preactivation [N][M]: what the forward pass left; NULL without an activation
  *   dX [N][D], dW [D][M], dbias [M] fp32: overwritten; any of them NULL to skip it.  X may be NULL without dW, W without dX.
