@@ -596,9 +596,16 @@ LUTNN_API const char* lutnn_last_error(void);
  *   "LUTNN_SMFMAC_ROW_GROUP"  "0" .. "64"               row tiles per group of its tile order (0 = plain)
  *   "LUTNN_SMFMAC_TILE_COLS"  "96" | "128"              width of its 512-row tiles
  *   "LUTNN_LOOKUP_F32"        "gather" | "rows" | "matrix"   which form the LDS variant runs on an fp32 table
+ *   "LUTNN_DENSE_FORM"        "few" | "memory" | "256x256" | "128x256" | "128x128" | "64x128" | "64x64" | "32x64" |
+ *                             "64x64 as is" | "32x64 as is" | "32x32 as is"   how the dense layers' products run: a few rows,
+ *                             fp32 straight from memory, or by tiles, of operands laid out or as they are
+ *   "LUTNN_DENSE_SPLITS"      "1" .. "64"               workgroups that share a sum of those products
+ *   "LUTNN_NORM_SUMS"         "beside" | "1" | "2"      layer norm's dweight and dbias: summed beside dX, or from that many
+ *                             workgroups per compute unit
  * value NULL or "" returns the switch to "not pinned".  A pinned choice the shape cannot take is
  * ignored.  Process-wide and atomic: safe to call while other threads launch, which then see
- * either the old or the new value.
+ * either the old or the new value.  The workspaces that lutnn_dense_linear*_workspace_bytes and
+ * lutnn_layer_norm_backward_workspace_bytes name are those of the switches at that time.
  * Errors: E_NULL (name), E_UNSUPPORTED (unknown name), E_SHAPE (value not understood).
  */
 LUTNN_API lutnn_status lutnn_set_tunable(const char* name, const char* value);

@@ -34,7 +34,8 @@ lutnn_status hip_result(hipError_t e, const char* what) {
 // ---- tuning switches (lutnn_kernels.h)
 const char* const kTunableNames[lutnn::kTuneCount] = {"LUTNN_FUSED_KERNEL", "LUTNN_SMFMAC_SPLIT",
                                                       "LUTNN_SMFMAC_TILE_ROWS", "LUTNN_SMFMAC_ROW_GROUP",
-                                                      "LUTNN_SMFMAC_TILE_COLS", "LUTNN_LOOKUP_F32"};
+                                                      "LUTNN_SMFMAC_TILE_COLS", "LUTNN_LOOKUP_F32", "LUTNN_DENSE_FORM",
+                                                      "LUTNN_DENSE_SPLITS", "LUTNN_NORM_SUMS"};
 std::atomic<int> g_tunable[lutnn::kTuneCount];
 std::once_flag g_tunable_once;
 
@@ -52,9 +53,20 @@ int parse_tunable(int which, const char* text) {
             if (std::strcmp(text, forms[i]) == 0) return i;
         return -1;
     }
+    if (which == lutnn::kTuneDenseForm) {
+        int i = 0;
+        for (const lutnn::DenseForm& form : lutnn::kDenseForms) {
+            if (std::strcmp(text, form.name) == 0) return i;
+            ++i;
+        }
+        return -1;
+    }
+    if (which == lutnn::kTuneNormSums && std::strcmp(text, "beside") == 0) return 0;
     char* end = nullptr;
     const long v = std::strtol(text, &end, 10);
     if (*end != 0) return -1;
+    if (which == lutnn::kTuneDenseSplits) return (v >= 1 && v <= 64) ? (int)v : -1;
+    if (which == lutnn::kTuneNormSums) return (v == 1 || v == 2) ? (int)v : -1;
     if (which == lutnn::kTuneSmfmacSplit) return (v == 0 || v == 1) ? (int)v : -1;
     if (which == lutnn::kTuneSmfmacRowGroup) return (v >= 0 && v <= 64) ? (int)v : -1;
     if (which == lutnn::kTuneSmfmacTileCols) return (v == 96 || v == 128) ? (int)v : -1;
@@ -1094,6 +1106,17 @@ lutnn_status check_dense(int32_t dtype, int64_t N, int32_t D, int32_t M, int32_t
     return LUTNN_OK;
 }
 
+// The switches are read once per call: the workspace that is asked for is that of what is launched.  A form that the call cannot take
+// is none; narrow: the columns of the narrowest operand whose rows do not run along k, a load's values at least in tiles as they are.
+lutnn::DenseCall dense_call(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int32_t D, int32_t M, int32_t narrow) {
+    int form = lutnn::tunable(lutnn::kTuneDenseForm);
+    if (form >= 0) {
+        const lutnn::DenseForm& f = lutnn::kDenseForms[form];
+        if (!(f.types & (dtype == LUTNN_F32 ? 1 : 2)) || (f.as_is && f.i > 0 && narrow < 16 / value_bytes(dtype))) form = -1;
+    }
+    return {dtype, X, N, ldx, W, ldw, D, M, form, lutnn::tunable(lutnn::kTuneDenseSplits)};
+}
+
 lutnn_status check_workspace(const void* workspace, size_t given, size_t needed) {
     if (needed == 0) return LUTNN_OK;
     if (!workspace) return fail(LUTNN_E_NULL, "workspace is NULL");
@@ -1125,7 +1148,7 @@ extern "C" {
 size_t lutnn_dense_linear_workspace_bytes(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int32_t D,
                                           int32_t M) {
     if (check_dense(dtype, N, D, M, LUTNN_ACTIVATION_NONE) || N == 0 || ldx < D || ldw < M) return 0;
-    return lutnn::dense_linear_workspace({dtype, X, N, ldx, W, ldw, D, M});
+    return lutnn::dense_linear_workspace(dense_call(dtype, X, N, ldx, W, ldw, D, M, M));
 }
 
 lutnn_status lutnn_dense_linear(int32_t dtype, const void* X, int64_t N, int64_t ldx, const void* W, int64_t ldw, int32_t D, int32_t M,
@@ -1140,7 +1163,7 @@ lutnn_status lutnn_dense_linear(int32_t dtype, const void* X, int64_t N, int64_t
                                         [&] { return check_matrix("preactivation", preactivation, ldz, M, dtype, false); },
                                         [&] { return check_vector("bias", bias); }))
         return st;
-    const lutnn::DenseCall call = {dtype, X, N, ldx, W, ldw, D, M};
+    const lutnn::DenseCall call = dense_call(dtype, X, N, ldx, W, ldw, D, M, M);
     if (lutnn_status st = check_workspace(workspace, workspace_bytes, lutnn::dense_linear_workspace(call))) return st;
     return hip_result(lutnn::launch_dense_linear(call, bias, activation, residual, ldr, Y, ldy, preactivation, ldz, workspace,
                                                  static_cast<hipStream_t>(stream)),
@@ -1153,7 +1176,7 @@ size_t lutnn_dense_linear_backward_workspace_bytes(int32_t dtype, const void* X,
                                                    int32_t need_dbias) {
     if (check_dense(dtype, N, D, M, activation) || N == 0) return 0;
     if (ldg < M || (activation && ldz < M) || (need_dx && ldw < M) || (need_dw && ldx < D)) return 0;
-    return lutnn::dense_linear_gradient_workspace({dtype, X, N, ldx, W, ldw, D, M}, G, ldg, preactivation, ldz, activation,
+    return lutnn::dense_linear_gradient_workspace(dense_call(dtype, X, N, ldx, W, ldw, D, M, std::min(D, M)), G, ldg, preactivation, ldz, activation,
                                                   need_dx != 0, need_dw != 0, need_dbias != 0);
 }
 
@@ -1170,7 +1193,7 @@ lutnn_status lutnn_dense_linear_backward(int32_t dtype, const void* X, int64_t N
                                         [&] { return check_matrix("dW", dW, lddw, M, dtype, false); },
                                         [&] { return check_vector("dbias", dbias); }))
         return st;
-    const lutnn::DenseCall call = {dtype, X, N, ldx, W, ldw, D, M};
+    const lutnn::DenseCall call = dense_call(dtype, X, N, ldx, W, ldw, D, M, std::min(D, M));
     if (N > 0)
         if (lutnn_status st = check_workspace(workspace, workspace_bytes,
                                               lutnn::dense_linear_gradient_workspace(call, G, ldg, preactivation, ldz, activation,
@@ -1202,7 +1225,7 @@ lutnn_status lutnn_layer_norm(int32_t dtype, const void* X, int64_t N, int64_t l
 
 size_t lutnn_layer_norm_backward_workspace_bytes(int64_t N, int32_t D) {
     if (check_norm(LUTNN_F32, N, D) || N == 0) return 0;
-    return lutnn::layer_norm_gradient_workspace(N, D);
+    return lutnn::layer_norm_gradient_workspace(N, D, lutnn::tunable(lutnn::kTuneNormSums));
 }
 
 lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int32_t D,
@@ -1219,11 +1242,12 @@ lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, 
                                         [&] { return check_vector("weight", weight); }, [&] { return check_vector("dweight", dweight); },
                                         [&] { return check_vector("dbias", dbias); }))
         return st;
+    const int sums = lutnn::tunable(lutnn::kTuneNormSums);
     if (dweight || dbias)
-        if (lutnn_status st = check_workspace(workspace, workspace_bytes, N > 0 ? lutnn::layer_norm_gradient_workspace(N, D) : 0)) return st;
+        if (lutnn_status st = check_workspace(workspace, workspace_bytes, N > 0 ? lutnn::layer_norm_gradient_workspace(N, D, sums) : 0)) return st;
     if (!dX && !dweight && !dbias) return LUTNN_OK;
     return hip_result(lutnn::launch_layer_norm_gradient(dtype, G, N, ldg, X, ldx, D, statistics, weight, residual, ldr, dX, lddx,
-                                                        dweight, dbias, workspace, static_cast<hipStream_t>(stream)),
+                                                        dweight, dbias, sums, workspace, static_cast<hipStream_t>(stream)),
                       "layer norm gradient launch");
 }
 

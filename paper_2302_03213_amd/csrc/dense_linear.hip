@@ -202,7 +202,7 @@ constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.3f}, {8.4f}},
                                   {128, 128, 32, 1, {2.02f}, {3.7f}},
                                   {64, 64, 32, 2, {1.08f, 2.07f}, {1.5f, 1.7f}, true},
                                   {32, 32, 32, 2, {0.32f, 0.56f}, {0.8f, 0.8f}, true}};
-constexpr float kLaunchUs = 3.5f;
+constexpr float kLaunchUs = 3.5f, kNever = 1e30f;
 
 // What sharing a sum out costs beside the shares: the second launch, and the shares written and read again, which of one 16-bit product
 // are in the caches more often.  64 x 4096 x 4096 in bf16 13.3 us by four, 17.1 by tiles of half the rows; both gradients' products
@@ -237,29 +237,50 @@ float tiles_us(const TileSize& t, float count, float stages, float units) {
     return us;
 }
 
+// What the switches allow of that; -1: anything.
+struct Pins {
+    int form, splits;
+    bool allows(const TileSize& t) const {
+        if (form <= kDenseMemory) return true;  // those are no tiles
+        const DenseForm& f = kDenseForms[form];
+        return f.i == t.i && f.j == t.j && f.as_is == t.as_is;
+    }
+};
+
+// The choice by `f` under the switches, without those that leave none.
+template <class F>
+auto pinned(const DenseCall& c, F&& f) {
+    auto best = f(Pins{c.form, c.splits});
+    if (best.us >= kNever && c.splits >= 0) best = f(Pins{c.form, -1});
+    if (best.us >= kNever && c.form >= 0) best = f(Pins{-1, -1});
+    return best;
+}
+
 // The fastest by those figures.  A sum is shared out where the last tiles would leave most of the chip idle for longer than a second
 // launch, which adds up what the first left in memory, takes.  k_rows: how many of the two operands run along k.
 // lay_out: us for that.
-Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out) {
+Plan plan(int dtype, int64_t I, int J, int64_t K, int k_rows, float lay_out, const Pins& pins) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 7, units = compute_units(), size = dtype == 0 ? 4 : 2;
     const int64_t narrow = k_rows == 2 ? 8 : k_rows == 1 ? J : std::min<int64_t>(I, J);  // of operands that do not run along k
     const Join join = dtype == 0 ? kJoin : kJoin16;
-    Plan best = {0, 0, 1, 0, 1e30f, false};
+    Plan best = {0, 0, 1, 0, kNever, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t tiles = ((I + t.i - 1) / t.i) * ((J + t.j - 1) / t.j), k_tiles = (K + t.depth - 1) / t.depth;
-        if (tiles > kMostTiles || (t.as_is && narrow < 16 / size)) continue;
+        if (tiles > kMostTiles || (t.as_is && narrow < 16 / size) || !pins.allows(t)) continue;
         const float stage = t.depth / 64.f, launch = kLaunchUs + (t.as_is ? 0.f : lay_out);
         // what tiles that read their operands as they are have on its way: 2 us for two stages of every workgroup
         const float bytes = t.as_is ? (float)(I + J) * K * size : 0.f, slots_bytes = (float)((t.i + t.j) * t.depth * size);
         const auto memory_us = [&](float workgroups) { return bytes / (std::min(workgroups, (float)units * t.at_once) * slots_bytes); };
         const float us = launch + std::max(tiles_us(t, (float)tiles, k_tiles * stage, (float)units), memory_us((float)tiles));
-        if (us < best.us) best = {i, (int)tiles, 1, tiles, us, t.as_is};
+        if (us < best.us && pins.splits <= 1) best = {i, (int)tiles, 1, tiles, us, t.as_is};
         const int64_t slots = units * t.at_once, whole = tiles / slots * slots, shared = tiles - whole;
         const float base = launch + join.us + tiles_us(t, (float)whole, k_tiles * stage, (float)units);
         if (shared == 0) continue;
-        for (const int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+        for (int splits : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (pins.splits == 1) break;
+            if (pins.splits > 1) splits = pins.splits;
             const float moved = base + 2.f * splits * shared * t.i * t.j * 4 / join.bytes_per_us;
             if (splits > k_tiles || moved >= best.us || shared * splits > kMostTiles) break;
             const float shared_us = moved + std::max(tiles_us(t, (float)shared * splits, (float)((k_tiles + splits - 1) / splits) * stage, (float)units),
@@ -278,21 +299,23 @@ struct PairPlan {
     bool as_is;
 };
 
-PairPlan pair_plan(int dtype, int64_t N, int D, int M, float lay_out) {
+PairPlan pair_plan(int dtype, int64_t N, int D, int M, float lay_out, const Pins& pins) {
     const TileSize* const sizes = dtype == 0 ? kTilesF32 : kTiles16;
     const int count = dtype == 0 ? 4 : 7;
     const float units = (float)compute_units();
     const Join join = kJoin;
-    PairPlan best = {0, 1, 1, 0, 0, 0, 1e30f, false};
+    PairPlan best = {0, 1, 1, 0, 0, 0, kNever, false};
     for (int i = 0; i < count; ++i) {
         const TileSize& t = sizes[i];
         const int64_t x_tiles = ((N + t.i - 1) / t.i) * ((D + t.j - 1) / t.j), w_tiles = ((int64_t)(D + t.i - 1) / t.i) * ((M + t.j - 1) / t.j);
-        if (std::max(x_tiles, w_tiles) > kMostTiles || (t.as_is && std::min(D, M) < (dtype == 0 ? 4 : 8))) continue;
+        if (std::max(x_tiles, w_tiles) > kMostTiles || (t.as_is && std::min(D, M) < (dtype == 0 ? 4 : 8)) || !pins.allows(t)) continue;
         const float x_stages = (float)((M + t.depth - 1) / t.depth), w_stages = (float)((N + t.depth - 1) / t.depth);
         const float unit = t.depth / 64.f, slots = units * t.at_once, tile_bytes = 8.f * t.i * t.j / join.bytes_per_us;
-        for (const int xs : {1, 2, 4}) {
+        for (int xs : {1, 2, 4}) {
+            if (pins.splits > 0) xs = pins.splits;
             if (xs > 1 && (xs > x_stages || x_tiles > slots)) break;
-            for (const int ws : {1, 2, 4, 8, 16, 32}) {
+            for (int ws : {1, 2, 4, 8, 16, 32}) {
+                if (pins.splits > 0) ws = pins.splits;
                 if (ws > 1 && (ws > w_stages || w_tiles * ws > 4 * slots)) break;
                 const float nx = (float)x_tiles * xs, nw = (float)w_tiles * ws;
                 const float kx = std::ceil(x_stages / xs) * unit, kw = std::ceil(w_stages / ws) * unit;
@@ -372,6 +395,11 @@ Operand operand(const void* given, int64_t ld, const uint16_t* laid_out, int64_t
     return o;
 }
 
+// Whether the way straight from memory, in `plain` us, is taken in place of tiles.
+bool plain_taken(const DenseCall& c, float plain, float tiles) {
+    return c.dtype == 0 && (c.form > kDenseFew ? c.form == kDenseMemory && plain < kNever : plain < tiles);
+}
+
 // What the backward pass has to have laid out, and its products: of both gradients in one launch, or of one.
 struct GradientPlan {
     bool plain, as_is;  // products of the operands as they are: fp32 ones without tiles, or either way
@@ -392,16 +420,16 @@ GradientPlan gradient_plan(const DenseCall& c, const void* G, int64_t ldg, int a
     // the pass over G is there for an activation or a bias either way; planes are half as much again to write
     const float lay_out = lay_out_us(c.dtype, values);
     if (g.both) {
-        g.pair = pair_plan(c.dtype, c.N, c.D, c.M, lay_out);
+        g.pair = pinned(c, [&](const Pins& p) { return pair_plan(c.dtype, c.N, c.D, c.M, lay_out, p); });
         tiles = g.pair.us, plain = plain_pair_us(c.N, c.D, c.M), g.as_is = g.pair.as_is;
     } else if (need_dx) {
-        g.one = plan(c.dtype, c.N, c.D, c.M, 2, lay_out);
+        g.one = pinned(c, [&](const Pins& p) { return plan(c.dtype, c.N, c.D, c.M, 2, lay_out, p); });
         tiles = g.one.us, plain = plain_f32_us(c.N, c.D, c.M), g.as_is = g.one.as_is;
     } else if (need_dw) {
-        g.one = plan(c.dtype, c.D, c.M, c.N, 0, lay_out);
+        g.one = pinned(c, [&](const Pins& p) { return plan(c.dtype, c.D, c.M, c.N, 0, lay_out, p); });
         tiles = g.one.us, plain = plain_f32_us(c.D, c.M, c.N), g.as_is = g.one.as_is;
     }
-    g.plain = c.dtype == 0 && plain < tiles;
+    g.plain = plain_taken(c, plain, tiles);
     g.as_is |= g.plain;
     g.x = !g.as_is && need_dw && !x_used;
     g.w = !g.as_is && need_dx && !w_used;
@@ -434,11 +462,12 @@ struct ForwardPlan {
 
 ForwardPlan forward_plan(const DenseCall& c) {
     ForwardPlan f = {};
-    f.few = few_rows(c.dtype, c.N, c.D, c.M);
+    f.few = c.form == kDenseFew ? c.N <= most_few_rows(c.dtype) : c.form < 0 && few_rows(c.dtype, c.N, c.D, c.M);
     if (f.few) return f;
     const bool x_used = usable(c.dtype, c.X, c.ldx, c.D), w_used = usable(c.dtype, c.W, c.ldw, c.M);
-    f.product = plan(c.dtype, c.N, c.M, c.D, 1, lay_out_us(c.dtype, (x_used ? 0.f : (float)c.N * c.D) + (w_used ? 0.f : (float)c.D * c.M)));
-    f.plain = c.dtype == 0 && plain_f32_us(c.N, c.M, c.D) < f.product.us;
+    const float lay_out = lay_out_us(c.dtype, (x_used ? 0.f : (float)c.N * c.D) + (w_used ? 0.f : (float)c.D * c.M));
+    f.product = pinned(c, [&](const Pins& p) { return plan(c.dtype, c.N, c.M, c.D, 1, lay_out, p); });
+    f.plain = plain_taken(c, plain_f32_us(c.N, c.M, c.D), f.product.us);
     f.x = !f.plain && !f.product.as_is && !x_used;
     f.w = !f.plain && !f.product.as_is && !w_used;
     return f;

@@ -10,6 +10,7 @@ constexpr int64_t kMostTiles = 1 << 21;
 // Whether N rows go through the kernel for single tokens.  fp32: four rows of 4096 x 4096 14 us, eight 17, five to sixteen by tiles
 // 23; eight of 1024 x 4096 8.0 and 7.7, of 4096 x 512 11 and 17, of 8192 x 1024 18.8 and 17.9.  16 bits: one row of 1024 x 4096 5.4,
 // two 6.3, four 8.4, two to sixteen by tiles 6.8; of 4096 x 4096 12.0, 13.5, 16.2 and 11.7.
+constexpr int most_few_rows(int dtype) { return dtype == 0 ? 8 : 2; }
 inline bool few_rows(int dtype, int64_t N, int D, int M) {
     const bool large = (int64_t)D * M >= 1 << 23;
     return N <= (dtype == 0 ? (large || D >= 2048 ? 8 : 4) : (large ? 1 : 2));

@@ -320,17 +320,19 @@ constexpr int64_t kDirectRows = 1024;
 // then), for rows whose loads keep the memory busy and for few rows beside wide sums: 4096 x 768 in fp32 9.2 us (one: 9.6, four: 11.0),
 // 16384 x 4096 in bf16 86 (one: 107), with a residual, 24 KB a row, 111 (one: 109), in fp32 with one, 48 KB, 211 (one: 199); 2048 x 3000
 // in bf16 23.4 (one: 22.2), 1536 x 4096 25.3 (one: 21.3), 3080 x 4096 29.9 (one: 30.7).
-int gradient_workgroups(int64_t N, int D, int64_t row_bytes = 0) {
-    const bool one = D > 256 * kValues || row_bytes >= 24 << 10 || (row_bytes > 0 && N <= 2048 && D > 2048);
+int gradient_workgroups(int64_t N, int D, int sums, int64_t row_bytes = 0) {
+    const bool one = sums > 0 ? sums == 1 : D > 256 * kValues || row_bytes >= 24 << 10 || (row_bytes > 0 && N <= 2048 && D > 2048);
     const int64_t most = (one ? 1 : 2) * (int64_t)compute_units();
     const int rows = rows_per_workgroup(D);
     return (int)std::min<int64_t>((N + rows - 1) / rows, most);
 }
 
+bool direct_sums(int64_t N, int sums) { return sums >= 0 ? sums == 0 : N <= kDirectRows; }
+
 }  // namespace
 
-size_t layer_norm_gradient_workspace(int64_t N, int D) {
-    return N <= kDirectRows ? 0 : (size_t)gradient_workgroups(N, D) * 2 * D * sizeof(float);
+size_t layer_norm_gradient_workspace(int64_t N, int D, int sums) {
+    return direct_sums(N, sums) ? 0 : (size_t)gradient_workgroups(N, D, sums) * 2 * D * sizeof(float);
 }
 
 hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
@@ -351,11 +353,11 @@ hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, i
 
 hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
                                       const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
-                                      float* dw, float* db, void* workspace, hipStream_t s) {
-    const bool direct = N <= kDirectRows && (dw || db);
+                                      float* dw, float* db, int sums, void* workspace, hipStream_t s) {
+    const bool direct = direct_sums(N, sums) && (dw || db);
     float* const partial = !direct && (dw || db) ? static_cast<float*>(workspace) : nullptr;
     const int64_t row_bytes = partial ? (int64_t)D * (dtype == 0 ? 4 : 2) * (R && dX ? 3 : 2) : 0;
-    const int groups = gradient_workgroups(N, D, row_bytes), rows = dX || partial ? groups : 0;
+    const int groups = gradient_workgroups(N, D, sums, row_bytes), rows = dX || partial ? groups : 0;
     if (groups > 0) {
         const hipError_t e = with_type(dtype, [&](auto t) {
             using T = decltype(t);

@@ -23,9 +23,28 @@ enum Tunable {
     kTuneSmfmacRowGroup,    // LUTNN_SMFMAC_ROW_GROUP: row tiles per group of the tile order, 0..64 (0 = plain)
     kTuneSmfmacTileCols,    // LUTNN_SMFMAC_TILE_COLS: 96 | 128, width of the 512-row tiles
     kTuneLookupF32,         // LUTNN_LOOKUP_F32: 0 = "gather", 1 = "rows", 2 = "matrix"
+    kTuneDenseForm,         // LUTNN_DENSE_FORM: an index of kDenseForms
+    kTuneDenseSplits,       // LUTNN_DENSE_SPLITS: 1..64
+    kTuneNormSums,          // LUTNN_NORM_SUMS: 0 = "beside", 1 | 2 = workgroups per compute unit
     kTuneCount
 };
 int tunable(int which);
+
+// The forms of a dense layer's products: few rows, fp32 straight from memory, and tiles of I rows by J columns, of operands that are
+// laid out or as they are.
+struct DenseForm {
+    const char* name;
+    int i, j;
+    bool as_is;
+    int types;  // 1: fp32, 2: 16 bits
+};
+constexpr int kDenseFew = 0, kDenseMemory = 1;
+constexpr DenseForm kDenseForms[] = {{"few", 0, 0, true, 3},           {"memory", 0, 0, true, 1},
+                                     {"256x256", 256, 256, false, 2},  {"128x256", 128, 256, false, 1},
+                                     {"128x128", 128, 128, false, 3},  {"64x128", 64, 128, false, 2},
+                                     {"64x64", 64, 64, false, 2},      {"32x64", 32, 64, false, 2},
+                                     {"64x64 as is", 64, 64, true, 3}, {"32x64 as is", 32, 64, true, 2},
+                                     {"32x32 as is", 32, 32, true, 1}};
 
 // Compute units of the current device (queried once per device; 256 on an MI355X).
 int compute_units();
@@ -203,7 +222,8 @@ hipError_t launch_linear_small_tree(const int32_t* split_dim, const float* thres
                                     const float* X, int64_t N, int64_t ldx, float* Y, int64_t ldy, hipStream_t s);
 
 // dense_linear.hip: a linear layer that is not looked up, Y = act(X W + b) + R, and its gradients.  dtype: lutnn_dtype;
-// activation: lutnn_activation.  Workspaces are 16-byte aligned.
+// activation: lutnn_activation.  Workspaces are 16-byte aligned.  form, splits: the switches as one call has read them, for its
+// workspace's size and its launches; -1: not pinned.
 struct DenseCall {
     int dtype;
     const void* X;
@@ -211,6 +231,7 @@ struct DenseCall {
     const void* W;
     int64_t ldw;
     int D, M;
+    int form = -1, splits = -1;
 };
 size_t dense_linear_workspace(const DenseCall& c);
 hipError_t launch_dense_linear(const DenseCall& c, const float* bias, int activation, const void* R, int64_t ldr, void* Y,
@@ -227,10 +248,11 @@ constexpr int kMaxNormWidth = 16384;
 hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
                              const float* b, float eps, void* Y, int64_t ldy, void* S, int64_t lds, float* statistics,
                              hipStream_t s);
-size_t layer_norm_gradient_workspace(int64_t N, int D);
+// sums: the switch LUTNN_NORM_SUMS
+size_t layer_norm_gradient_workspace(int64_t N, int D, int sums);
 hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
                                       const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
-                                      float* dw, float* db, void* workspace, hipStream_t s);
+                                      float* dw, float* db, int sums, void* workspace, hipStream_t s);
 
 // probe_smfmac.hip: sink holds 256 * compute_units() ints
 hipError_t launch_probe_smfmac_stream(int operands, int iterations, int32_t* sink, hipStream_t s);
