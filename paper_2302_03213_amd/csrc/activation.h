@@ -73,14 +73,6 @@ __device__ __forceinline__ void with_activation(int activation, F&& f) {
     }
 }
 
-template <int n>
-__device__ __forceinline__ void activate_all(float (&z)[n], int activation) {
-    with_activation(activation, [&](auto kind) {
-#pragma unroll
-        for (int r = 0; r < n; ++r) z[r] = activate(z[r], decltype(kind)::value);
-    });
-}
-
 // g times the slopes at z
 template <int n>
 __device__ __forceinline__ void slope_all(float (&g)[n], const float (&z)[n], int activation) {
