@@ -545,7 +545,7 @@ LUTNN_API lutnn_status lutnn_layer_norm(int32_t dtype, const void* X, int64_t N,
  *
  *   residual [N][D] or NULL: a gradient that reaches X by another way, as where the total goes on beside the norm
  *   dX [N][D], dweight [D], dbias [D] fp32: overwritten; any of them NULL to skip it.  N == 0: dweight and dbias are zeros.
- *   workspace  for dweight and dbias; few rows need none, as the query says
+ *   workspace  for dweight and dbias; few rows need none, as the query, which is for the type that needs most, says
  * Errors: as lutnn_layer_norm.
  */
 LUTNN_API lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx,

@@ -1225,7 +1225,7 @@ lutnn_status lutnn_layer_norm(int32_t dtype, const void* X, int64_t N, int64_t l
 
 size_t lutnn_layer_norm_backward_workspace_bytes(int64_t N, int32_t D) {
     if (check_norm(LUTNN_F32, N, D) || N == 0) return 0;
-    return lutnn::layer_norm_gradient_workspace(N, D, lutnn::tunable(lutnn::kTuneNormSums));
+    return lutnn::layer_norm_gradient_workspace(LUTNN_F32, N, D, lutnn::tunable(lutnn::kTuneNormSums));
 }
 
 lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int32_t D,
@@ -1244,7 +1244,7 @@ lutnn_status lutnn_layer_norm_backward(int32_t dtype, const void* G, int64_t N, 
         return st;
     const int sums = lutnn::tunable(lutnn::kTuneNormSums);
     if (dweight || dbias)
-        if (lutnn_status st = check_workspace(workspace, workspace_bytes, N > 0 ? lutnn::layer_norm_gradient_workspace(N, D, sums) : 0)) return st;
+        if (lutnn_status st = check_workspace(workspace, workspace_bytes, N > 0 ? lutnn::layer_norm_gradient_workspace(dtype, N, D, sums) : 0)) return st;
     if (!dX && !dweight && !dbias) return LUTNN_OK;
     return hip_result(lutnn::launch_layer_norm_gradient(dtype, G, N, ldg, X, ldx, D, statistics, weight, residual, ldr, dX, lddx,
                                                         dweight, dbias, sums, workspace, static_cast<hipStream_t>(stream)),

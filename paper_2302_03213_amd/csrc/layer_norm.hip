@@ -315,28 +315,38 @@ hipError_t by_width(int D, F&& f) {
 
 int rows_per_workgroup(int D) { return D <= 16 * kValues ? kThreads / 16 : D <= 64 * kValues ? kThreads / 64 : 1; }
 
-// Few rows are read again for dw and db beside dX, and not summed by workgroup and then over those: 256 x 768 6.0 us for 9.8,
-// 256 x 4096 in fp32 6 for 13 (bf16 6 for 15), 1024 x 4096 22 for 20 (14 for 26), 1024 x 16384 67 for 94 (33 for 56), 1536 x 4096 32 for
-// 23 (21 for 25).
-constexpr int64_t kDirectRows = 1024;
+// Few rows are read again for dw and db beside dX, and not summed by workgroup and then over those.  us so and the other way, by rows:
+//   fp32   1024 x 1032 11.0, 12.0;  896 x 2048 12.0, 13.5;  1024 x 2048 13.8, 13.8 (with a residual 17.1, 13.9);  768 x 3000 14.0, 15.1;
+//          896 x 3000 17.1, 16.3;  768 x 4096 16.2, 16.5;  1024 x 4096 23.3, 18.9;  1024 x 5120 19.8, 19.8;  1024 x 16384 68, 94
+//   bf16   1024 x 1032 7.7, 11.9;  1024 x 2048 10.1, 13.8;  1024 x 4096 15.2, 20.5;  1024 x 5120 13.9, 21.4;  1024 x 16384 33, 57
+// Above 4096 values a workgroup has more threads, and takes more columns.  From 1025 rows on both ways are near each other at most
+// widths: 1536 x 1024 12.9, 10.6 (bf16 10.2, 10.7), 1536 x 4096 32, 21 (21, 21), 1536 x 8192 38, 33 (27, 30).
+int64_t direct_rows(int dtype, int D) { return dtype == 0 && D > 2048 && D <= 256 * kValues ? 768 : 1024; }
 
 // Two workgroups per compute unit; one for rows of more than four wavefronts, and, where sums are left (row_bytes: what a row reads
-// then), for rows whose loads keep the memory busy and for few rows beside wide sums: 4096 x 768 in fp32 9.2 us (one: 9.6, four: 11.0),
-// 16384 x 4096 in bf16 86 (one: 107), with a residual, 24 KB a row, 111 (one: 109), in fp32 with one, 48 KB, 211 (one: 199); 2048 x 3000
-// in bf16 23.4 (one: 22.2), 1536 x 4096 25.3 (one: 21.3), 3080 x 4096 29.9 (one: 30.7).
+// then), where the memory is what they wait for, and for few rows beside wide sums.  us by one and by two:
+//   6 KB (bf16, 1024 wide, a residual)  4096 rows 12.4, 13.4;  16384 28.7, 27.1       12 KB (fp32, 1536)  4096 26.4, 20.2;  16384 84, 62
+//   16 KB (bf16, 4096)  4096 35.9, 33.4;  16384 106, 86                               23.5 KB (fp32, 3008)  8192 55.3, 53.0;  16384 107, 116
+//   24 KB (bf16, 4096, a residual)  4096 37.2, 36.6;  8192 60.9, 54.0;  16384 109, 110
+//         (fp32, 2048, a residual)  4096 28.6, 27.7;  8192 48.6, 45.2;  16384 95.9, 101.6
+//   28 KB (fp32, 3584)  4096 35.2, 35.6;  16384 136, 140          30 KB (fp32, 2560, a residual)  4096 31.8, 32.6;  16384 125, 133
+//   48 KB (fp32, 4096, a residual)  4096 47.1, 49.0;  16384 199, 209
+// so at 24 KB it is one where G, X and the residual pass the 256 MB cache.  Few rows: 2048 x 3008 in bf16 21.6, 22.2, 2048 x 4096 24.0,
+// 26.8 (fp32 24.5, 26.2), 1100 x 2560 16.5, 19.1, but 2048 x 2560 in fp32 20.0, 19.1, and 3080 x 4096 30.6, 29.8.
 int gradient_workgroups(int64_t N, int D, int sums, int64_t row_bytes = 0) {
-    const bool one = sums > 0 ? sums == 1 : D > 256 * kValues || row_bytes >= 24 << 10 || (row_bytes > 0 && N <= 2048 && D > 2048);
+    const bool busy = row_bytes > 24 << 10 || (row_bytes == 24 << 10 && N * row_bytes > 256 << 20);
+    const bool one = sums > 0 ? sums == 1 : D > 256 * kValues || busy || (row_bytes > 0 && N <= 2048 && D > 2048);
     const int64_t most = (one ? 1 : 2) * (int64_t)compute_units();
     const int rows = rows_per_workgroup(D);
     return (int)std::min<int64_t>((N + rows - 1) / rows, most);
 }
 
-bool direct_sums(int64_t N, int sums) { return sums >= 0 ? sums == 0 : N <= kDirectRows; }
+bool direct_sums(int dtype, int64_t N, int D, int sums) { return sums >= 0 ? sums == 0 : N <= direct_rows(dtype, D); }
 
 }  // namespace
 
-size_t layer_norm_gradient_workspace(int64_t N, int D, int sums) {
-    return direct_sums(N, sums) ? 0 : (size_t)gradient_workgroups(N, D, sums) * 2 * D * sizeof(float);
+size_t layer_norm_gradient_workspace(int dtype, int64_t N, int D, int sums) {
+    return direct_sums(dtype, N, D, sums) ? 0 : (size_t)gradient_workgroups(N, D, sums) * 2 * D * sizeof(float);
 }
 
 hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
@@ -358,7 +368,7 @@ hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, i
 hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
                                       const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
                                       float* dw, float* db, int sums, void* workspace, hipStream_t s) {
-    const bool direct = direct_sums(N, sums) && (dw || db);
+    const bool direct = direct_sums(dtype, N, D, sums) && (dw || db);
     float* const partial = !direct && (dw || db) ? static_cast<float*>(workspace) : nullptr;
     const int64_t row_bytes = partial ? (int64_t)D * (dtype == 0 ? 4 : 2) * (R && dX ? 3 : 2) : 0;
     const int groups = gradient_workgroups(N, D, sums, row_bytes), rows = dX || partial ? groups : 0;

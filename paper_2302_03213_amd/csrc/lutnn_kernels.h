@@ -248,8 +248,8 @@ constexpr int kMaxNormWidth = 16384;
 hipError_t launch_layer_norm(int dtype, const void* X, int64_t N, int64_t ldx, int D, const void* R, int64_t ldr, const float* w,
                              const float* b, float eps, void* Y, int64_t ldy, void* S, int64_t lds, float* statistics,
                              hipStream_t s);
-// sums: the switch LUTNN_NORM_SUMS
-size_t layer_norm_gradient_workspace(int64_t N, int D, int sums);
+// sums: the switch LUTNN_NORM_SUMS.  fp32 needs a workspace wherever the other types do.
+size_t layer_norm_gradient_workspace(int dtype, int64_t N, int D, int sums);
 hipError_t launch_layer_norm_gradient(int dtype, const void* G, int64_t N, int64_t ldg, const void* X, int64_t ldx, int D,
                                       const float* statistics, const float* w, const void* R, int64_t ldr, void* dX, int64_t lddx,
                                       float* dw, float* db, int sums, void* workspace, hipStream_t s);
