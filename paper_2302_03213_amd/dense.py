@@ -53,13 +53,14 @@ class _DenseLinearFn(torch.autograd.Function):
 
 class DenseLinear(torch.nn.Module):
     """activation(X @ W + bias) + residual, with W [D, M] and bias [M] learned.  X [N, D], W and the residual have one type (fp32,
-    bf16, fp16), the bias is fp32; activation None, "relu", "gelu", "gelu_tanh" or "silu"."""
+    bf16, fp16), the bias is fp32; activation None, "relu", "gelu", "gelu_tanh" or "silu".  W is copied row by row, so that a
+    torch.nn.Linear's weight.t() will do."""
 
     def __init__(self, W, bias=None, activation=None):
         super().__init__()
         _b._activation(activation)
-        self.W = torch.nn.Parameter(W.detach().clone())
-        self.bias = None if bias is None else torch.nn.Parameter(bias.detach().clone())
+        self.W = torch.nn.Parameter(W.detach().clone(memory_format=torch.contiguous_format))
+        self.bias = None if bias is None else torch.nn.Parameter(bias.detach().clone(memory_format=torch.contiguous_format))
         self.activation = activation
 
     def forward(self, X, residual=None):
