@@ -543,6 +543,8 @@ LUTNN_API lutnn_status lutnn_layer_norm(int32_t dtype, const void* X, int64_t N,
  *   h = (X - mean) rstd,  q = G weight:   dX = rstd (q - sum_d q / D - h sum_d (q h) / D) + residual,
  *   dweight = sum_n G h,  dbias = sum_n G
  *
+ *   A total of 16 bits is rounded and the statistics are those of what was not: h is then off by half a step of X times rstd at
+ *   most, against the h that Y was made of.  That weighs where a row's mean is large against its spread.
  *   residual [N][D] or NULL: a gradient that reaches X by another way, as where the total goes on beside the norm
  *   dX [N][D], dweight [D], dbias [D] fp32: overwritten; any of them NULL to skip it.  N == 0: dweight and dbias are zeros.
  *   workspace  for dweight and dbias; few rows need none, as the query, which is for the type that needs most, says

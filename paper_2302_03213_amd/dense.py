@@ -92,7 +92,8 @@ class _LayerNormFn(torch.autograd.Function):
 
 class LayerNorm(torch.nn.Module):
     """The norm of X + residual over rows of D values, with weight and bias [D] learned (fp32).  forward(X, residual) gives Y;
-    forward(X, residual, with_total=True) gives (Y, X + residual)."""
+    forward(X, residual, with_total=True) gives (Y, X + residual).  With a residual the backward pass goes by the sum as it was kept,
+    rounded to X's type: lutnn_layer_norm_backward says what that is off by."""
 
     def __init__(self, D, eps=1e-5, device="cuda"):
         super().__init__()
