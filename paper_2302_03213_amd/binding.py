@@ -761,7 +761,7 @@ def _workspace(nbytes, like):
 def dense_linear(X, W, bias=None, activation=None, residual=None, out=None, preactivation=None):
     """lutnn_dense_linear: Y = activation(X @ W + bias) + residual.  X [N, D], W [D, M] and residual [N, M] of one type (fp32,
     bf16, fp16), bias [M] fp32; activation None, "relu", "gelu", "gelu_tanh" or "silu".  preactivation: an [N, M] tensor that
-    receives X @ W + bias, as dense_linear_backward wants it."""
+    receives X @ W + bias, as dense_linear_backward wants it.  What is written must not overlap what is read."""
     if out is None:
         got = _calls.dense_linear(X, W, bias, ACTIVATIONS.get(activation, -1), residual, preactivation)
         if got is not None:
@@ -812,7 +812,8 @@ def dense_linear_backward(X, W, G, preactivation=None, activation=None, need_dx=
 def layer_norm(X, weight=None, bias=None, eps=1e-5, residual=None, out=None, total=None, statistics=None):
     """lutnn_layer_norm: the rows of S = X + residual, normalised, times weight, plus bias.  X [N, D] and residual of one type
     (fp32, bf16, fp16), weight and bias [D] fp32.  total: an [N, D] tensor that receives S; statistics: an [N, 2] fp32 tensor that
-    receives the rows' mean and 1 / sqrt(variance + eps), as layer_norm_backward wants them."""
+    receives the rows' mean and 1 / sqrt(variance + eps), as layer_norm_backward wants them.  What is written must not overlap what
+    is read: total is neither X nor the residual."""
     if out is None:
         got = _calls.layer_norm(X, weight, bias, eps, residual, total, statistics)
         if got is not None:

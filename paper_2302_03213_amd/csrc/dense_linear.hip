@@ -185,7 +185,9 @@ hipError_t launch_clear(int dtype, void* dW, int64_t ld, int D, int M, float* db
 // 64 k, and beside that.  16 bits: from products of 16 x 16 n tiles at K = 512 and 2560, the three layouts' average.  Small tiles are
 // bound by what a compute unit gets from L2 (75 GB/s), the large ones by the matrix instructions and the power they draw.  fp32: fitted
 // to the times of 28 sizes from 8 x 768 x 768 to 4096 x 4096 x 768, three products each, which they then order so that the choice
-// takes 2 % longer than the best of all; tiles of 64 x 64 and 64 x 128 from planes were the best of none by more than 1 %.
+// takes 2 % longer than the best of all; tiles of 64 x 64 and 64 x 128 from planes were the best of none by more than 1 %.  At 56 sizes
+// that nothing was fitted to, 24 to 6000 rows by widths of 512 to 4608, the choice takes 3 % longer than the best tile (forward, both
+// gradients and dW alone; at worst 40 %, both gradients of 24 x 640 x 2560), in bf16 1, 4 and 2 % (69 %, those of 24 x 4608 x 1152).
 struct TileSize {
     int i, j, depth, at_once;
     float stage[4], rest[4];
@@ -204,9 +206,9 @@ constexpr TileSize kTilesF32[] = {{128, 256, 32, 1, {3.3f}, {8.4f}},
                                   {32, 32, 32, 2, {0.32f, 0.56f}, {0.8f, 0.8f}, true}};
 constexpr float kLaunchUs = 3.5f, kNever = 1e30f;
 
-// What sharing a sum out costs beside the shares: the second launch, and the shares written and read again, which of one 16-bit product
-// are in the caches more often.  64 x 4096 x 4096 in bf16 13.3 us by four, 17.1 by tiles of half the rows; both gradients' products
-// chosen so took up to 14 % longer.
+// What sharing a sum out costs beside the shares: the second launch, and the shares written and read again.  One 16-bit product's are set
+// by what they choose, not timed by themselves: 64 x 4096 x 4096 in bf16 13.3 us by four, 17.1 by tiles of half the rows, as kJoin has
+// it; both gradients' products chosen by kJoin16 took up to 14 % longer.
 struct Join {
     float us, bytes_per_us;
 };
